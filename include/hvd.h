@@ -24,6 +24,9 @@
  *  - Variants of the three steps (two-layer and extended predictors, token
  *    trees, frequency-weighted drafts, a shared warm-up corpus, vocabulary
  *    shards, trace replay) are declared next to the step they vary.
+ *  - Of the target forward the library has the part that works on the paged
+ *    key/value cache, in the chunk layout of the verification:
+ *    hvd_set_attention, hvd_rope_append, hvd_attn_paged, hvd_kv_commit.
  *  - Errors the host can see (NULL pointer, sizes outside the limits given at
  *    hvd_create, unknown dtype, misaligned base pointer) are returned at once
  *    and nothing is enqueued.  Data-dependent problems are reported per
@@ -46,8 +49,8 @@
  *    must have written them before it does.
  *    Results do not depend on it.  One environment
  *    variable, read once by hvd_create, changes it: HVD_PDL_MASK (a bit per
- *    kernel pair: 1 commit, 2 lookup, 4 verify stream, 8 scoring; default 15,
- *    0 = plain launches).  It exists for the tests, which run the parity
+ *    kernel pair: 1 commit, 2 lookup, 4 verify stream, 8 scoring, 16 the cache
+ *    operators; default 31, 0 = plain launches).  It exists for the tests, which run the parity
  *    cases with and without the overlap.
  *  - hvd_verify_commit and its variants stream the logits with one of two
  *    kernels, chosen by the size of the logits: one warp per 4 KB batch of a
@@ -94,13 +97,18 @@ typedef enum {
     HVD_ERR_ALLOC = 4
 } hvd_status;
 
-typedef enum { HVD_F32 = 0, HVD_BF16 = 1 } hvd_dtype;
+typedef enum {
+    HVD_F32 = 0,
+    HVD_BF16 = 1,
+    HVD_F16 = 2 /* the cache operators only (hvd_set_attention) */
+} hvd_dtype;
 
 /* written per request, on the device, by hvd_verify_commit */
 typedef enum {
     HVD_REQ_OK = 0,
     HVD_REQ_CAPACITY = 1, /* slab too small: commit clamped to the free space */
-    HVD_REQ_BAD_LEN = 2   /* hist_len outside [0, hist_cap] or no logits rows: request skipped */
+    HVD_REQ_BAD_LEN = 2,  /* hist_len outside [0, hist_cap] or no logits rows: request skipped */
+    HVD_REQ_BAD_PAGE = 3  /* cache operators: an entry of the page table lies outside the pool */
 } hvd_req_status;
 
 /* values of the device status word (hvd_device_status) */
@@ -555,6 +563,151 @@ HVD_API hvd_status hvd_verify_commit_noalloc(int32_t B, int32_t k_cap, const voi
                                              int32_t* status, void* stream);
 /* text of the last error of hvd_verify_commit_noalloc on the calling thread ("" if none) */
 HVD_API const char* hvd_noalloc_last_error(void);
+
+/*
+ * ---------------------------------------------------------------------------------------------------
+ * The target forward's work on the key/value cache.  (The paper leaves the target model to its serving
+ * engine, Sec. 3.1; these operators take the engine's place around hvd_verify_commit.)
+ *
+ * A CHUNK is what one decoding step hands to the target model.  Request b owns rows [r0, r1) exactly as in
+ * hvd_verify_commit (row_off, or k_uniform), of which n_new = min(sel_len[b], k_cap, r1 - r0 - 1) + 1 are new
+ * tokens: row r0 is the last committed token, row r0 + i its i-th draft token.  sel_len = NULL: every row is
+ * a new token (n_new = r1 - r0, also 0), whatever their number: a piece of a prompt.  cache_len[b] tokens are
+ * cached already; row r0 + i takes cache slot cache_len[b] + i.
+ * Chain (parent = NULL): row i follows row i-1.  Tree (parent as in hvd_verify_commit_tree, needs sel_len):
+ * row i + 1 is node i and follows node parent[b, i] (-1: the root, row r0).  A node whose line of parents
+ * leaves {-1, 0 .. i-1} is unreachable: its position is that of the root and it sees nothing.
+ *
+ * The cache of one layer is a pool of pages.  Element e of head h of slot s of page p is at
+ *   p * page_stride + s * slot_stride + h * head_stride + e     (strides in elements, the same for k and v),
+ * so [page, slot, head, e] and [page, head, slot, e] arrays both fit.  Token t of request b lies in slot
+ * t % page_size of page page_table[b * table_stride + t / page_size].  page_size is a multiple of 8; bases
+ * are 16-byte aligned, strides multiples of 8 elements, so that TMA can fetch the pages.
+ * A request with cache_len < 0, cache_len + n_new > table_stride * page_size, rows outside
+ * [0, total_rows) or (sel_len given) no row is skipped: status HVD_REQ_BAD_LEN.
+ * ---------------------------------------------------------------------------------------------------
+ */
+
+/* which two elements of a head turn together: i and i + rot_dim/2, or 2i and 2i + 1 */
+typedef enum { HVD_ROPE_HALVES = 0, HVD_ROPE_PAIRS = 1 } hvd_rope_layout;
+
+/* Long-context scaling of w_i = rope_base^(-2i / rot_dim), i in [0, rot_dim/2):
+ *   PLAIN   w_i
+ *   LINEAR  w_i / factor (positions interpolated)
+ *   BASE    w_i with rope_base * factor^(rot_dim / (rot_dim - 2)) (needs rot_dim > 2)
+ *   PARTS   g_i w_i + (1 - g_i) w_i / factor, g_i = 1 - clamp((i - lo) / max(hi - lo, 1/1000), 0, 1);
+ *           lo = max(floor(I(rope_high)), 0), hi = min(ceil(I(rope_low)), rot_dim - 1), I(t) = the (fractional) i
+ *           whose pair makes t turns within rope_original_len positions
+ *   BANDS   the same mix, g_i = clamp((t_i - rope_low) / (rope_high - rope_low), 0, 1), t_i = the turns of pair i
+ *           within rope_original_len positions
+ * cos and sin are multiplied by rope_magnitude in every form. */
+typedef enum { HVD_ROPE_PLAIN = 0, HVD_ROPE_LINEAR = 1, HVD_ROPE_BASE = 2, HVD_ROPE_PARTS = 3, HVD_ROPE_BANDS = 4 } hvd_rope_scaling;
+
+enum { HVD_MAX_HEAD_DIM = 128, HVD_MAX_HEAD_GROUP = 128 };
+
+typedef struct {
+    int32_t n_q_heads;     /* a multiple of n_kv_heads, at most HVD_MAX_HEAD_GROUP times as many */
+    int32_t n_kv_heads;    /* >= 1; query head h reads key/value head h / (n_q_heads / n_kv_heads) */
+    int32_t head_dim;      /* a multiple of 8, 8 .. HVD_MAX_HEAD_DIM */
+    int32_t dtype;         /* HVD_BF16 or HVD_F16: q, k, v, out and the cache */
+    float softmax_scale;   /* > 0; 0 stands for 1 / sqrt(head_dim) */
+    int32_t rot_dim;       /* leading elements of each head that are rotated: even, 0 .. head_dim */
+    int32_t rot_layout;    /* hvd_rope_layout */
+    int32_t rope_scaling;  /* hvd_rope_scaling */
+    double rope_base;      /* > 1 */
+    double rope_factor;    /* >= 1 (LINEAR, BASE, PARTS, BANDS) */
+    double rope_original_len; /* > 0 (PARTS, BANDS) */
+    double rope_low;       /* 0 < rope_low < rope_high (PARTS, BANDS): turns */
+    double rope_high;
+    double rope_magnitude; /* > 0; 0 stands for 1 */
+} hvd_attn_config;
+
+typedef struct {
+    void* k;                   /* DEVICE */
+    void* v;                   /* DEVICE */
+    int64_t n_pages;           /* pages of the pool, 1 .. 2^31 - 1 */
+    int32_t page_size;         /* a multiple of 8, 8 .. 65536 */
+    int32_t table_stride;      /* entries per request in page_table, >= 1; table_stride * page_size < 2^31 */
+    const int32_t* page_table; /* DEVICE int32 [B, table_stride] */
+    int64_t page_stride, slot_stride, head_stride; /* in elements, multiples of 8, > 0 */
+} hvd_kv_cache;
+
+/* Rows of heads: element e of head h of row r is at p + r * row_stride + h * head_stride + e (strides in
+   elements, multiples of 8; p DEVICE, 16-byte aligned), e.g. a slice of a fused projection's output. */
+typedef struct {
+    void* p;
+    int64_t row_stride, head_stride;
+} hvd_heads;
+
+/* The angular frequencies that hvd_rope_append uses (all HOST; no device needed): freq[rot_dim / 2], and the
+   factor on cos and sin in *magnitude.  HVD_ERR_INVALID_ARG if cfg is not one that hvd_set_attention takes. */
+HVD_API hvd_status hvd_rope_frequencies(const hvd_attn_config* cfg, double* freq, double* magnitude);
+
+/* Stores the attention geometry and allocates the operators' scratch (partial results of rows whose keys are
+   split over several SMs: two slots of 256 rows per SM, about 39 MB at head_dim 128).  A set-up call: it
+   waits for the device and is not for stream capture; no operator of this context may be in flight. */
+HVD_API hvd_status hvd_set_attention(hvd_ctx* ctx, const hvd_attn_config* cfg);
+
+/*
+ * Rotary positions and cache append.  For every new token (row i of the chunk, position
+ * t = cache_len[b] + i, or + the node's depth in a tree): with a = t * w_j, (c, s) = rope_magnitude * (cos a, sin a),
+ * each rotated pair (x, y) of its q and k heads becomes (x c - y s, x s + y c); the other elements stay as they are.
+ * q goes to q_out, k and v to the token's cache slot.  Angles are right to 2^-26 of a turn at every position;
+ * the products are in 32 bits and rounded once.  Rows that are no new token are neither read nor written.
+ * A token whose page entry lies outside [0, n_pages) is not cached: status HVD_REQ_BAD_PAGE (its q_out is written).
+ *
+ * q, k, v  HOST structs: [total_rows] rows of n_q_heads, n_kv_heads, n_kv_heads heads
+ * q_out    HOST struct; may be the same array as q (same strides)
+ * status   int32 [B], DEVICE output: HVD_REQ_OK, HVD_REQ_BAD_LEN, HVD_REQ_BAD_PAGE
+ */
+HVD_API hvd_status hvd_rope_append(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, const int32_t* cache_len,
+                                   const int64_t* row_off, int32_t k_uniform, int64_t total_rows,
+                                   const int32_t* sel_len, const int32_t* parent, const hvd_heads* q,
+                                   const hvd_heads* k, const hvd_heads* v, const hvd_heads* q_out, int32_t* status,
+                                   void* stream);
+
+/*
+ * Attention of a chunk's rows over the paged cache, which holds the chunk itself (hvd_rope_append).  Row i of
+ * request b sees the cache_len[b] tokens before the chunk and, in a chain, rows 0..i of the chunk; in a tree
+ * itself, its ancestors and the root.  Per query head, with x_j = softmax_scale * q . k_j over what is seen:
+ *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j)
+ * Scores, statistics and sums are in 32 bits; the weights exp(x_j - running maximum) are rounded to the cache's
+ * type for the product with v.  Rows that see nothing (rows beyond n_new, unreachable nodes, skipped
+ * requests) get out = 0 and lse = -inf; rows of no request are not written.  Slots at and behind cache_len + n_new may hold anything, also NaN.  The
+ * k and v of tokens below that have to be finite: a row's zero weight times an infinite v is NaN.
+ * A page entry outside [0, n_pages) stands for a page of zeros.
+ *
+ * q    HOST struct, [total_rows] rows of n_q_heads heads
+ * out  HOST struct, the same shape; another array than q
+ * lse  float [total_rows, n_q_heads], DEVICE output, natural logarithm; may be NULL
+ * status int32 [B], DEVICE output: HVD_REQ_OK or HVD_REQ_BAD_LEN; may be NULL
+ * Uses context scratch: one call at a time per context.
+ */
+HVD_API hvd_status hvd_attn_paged(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, const int32_t* cache_len,
+                                  const int64_t* row_off, int32_t k_uniform, int64_t total_rows,
+                                  const int32_t* sel_len, const int32_t* parent, const hvd_heads* q,
+                                  const hvd_heads* out, float* lse, int32_t* status, void* stream);
+
+/*
+ * The cache's side of a commit: after the verification of a chunk, new_len[b] = cache_len[b] + n_commit[b]
+ * tokens of the cache are history (the root and the accepted draft tokens; the last committed token is the
+ * next chunk's root).  For a tree (parent != NULL) the accepted nodes' slots are first made consecutive: the
+ * j-th accepted node (j = 0 .. min(accepted, n_commit - 1) - 1) goes from slot cache_len + 1 + node to slot
+ * cache_len + 1 + j, in every layer.  The path is the one that hvd_verify_commit_tree took: from the root, the child of
+ * lowest index that carries the next token of `committed`.  Where the path ends early (outputs of another
+ * call) or an entry of the page table lies outside the pool, the rest of the request's nodes stays where it is.
+ *
+ * cache        the first layer's; layer l's arrays start l * layer_stride elements (a multiple of 8) further on
+ * sel_draft, parent int32 [B, k_cap]; sel_len, accepted, n_commit int32 [B]; committed int32 [B, k_cap + 1]:
+ *              hvd_verify_commit_tree's arguments and outputs.  Chain: parent = NULL, and sel_draft, sel_len,
+ *              accepted and committed may be NULL; nothing is moved
+ * new_len      int32 [B], DEVICE output; may be cache_len itself.  A request with n_commit <= 0, cache_len < 0 or
+ *              cache_len + n_commit beyond its table keeps its length and its slots
+ */
+HVD_API hvd_status hvd_kv_commit(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int32_t n_layers,
+                                 int64_t layer_stride, const int32_t* cache_len, const int32_t* parent,
+                                 const int32_t* sel_draft, const int32_t* sel_len, const int32_t* accepted,
+                                 const int32_t* committed, const int32_t* n_commit, int32_t* new_len, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,12 +12,14 @@ import numpy as np
 
 from . import build as _build
 
-F32, BF16 = 0, 1
-REQ_OK, REQ_CAPACITY, REQ_BAD_LEN = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
+REQ_OK, REQ_CAPACITY, REQ_BAD_LEN, REQ_BAD_PAGE = 0, 1, 2, 3
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS, ROPE_BANDS = 0, 1, 2, 3, 4
 N_FEATURES = 8
 STATE_DTYPE = np.dtype([("sel_bits", "<u4"), ("pad", "<u4"), ("acc_ring", "<u8")])
 
-_vp, _i32, _i64, _f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+_vp, _i32, _i64, _f32, _f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double
 
 
 class HvdError(RuntimeError):
@@ -44,6 +46,22 @@ class HvdHostStepArgs(C.Structure):
                 ("k_uniform", _i32), ("V", _i64), ("row_off", _vp), ("total_rows", _i64),
                 ("score", _vp), ("select", _vp), ("sel_draft", _vp), ("sel_len", _vp), ("accepted", _vp),
                 ("committed", _vp), ("n_commit", _vp), ("status", _vp)]
+
+
+class HvdAttnConfig(C.Structure):
+    _fields_ = [("n_q_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("dtype", _i32),
+                ("softmax_scale", _f32), ("rot_dim", _i32), ("rot_layout", _i32), ("rope_scaling", _i32),
+                ("rope_base", _f64), ("rope_factor", _f64), ("rope_original_len", _f64), ("rope_low", _f64),
+                ("rope_high", _f64), ("rope_magnitude", _f64)]
+
+
+class HvdKvCache(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("n_pages", _i64), ("page_size", _i32), ("table_stride", _i32),
+                ("page_table", _vp), ("page_stride", _i64), ("slot_stride", _i64), ("head_stride", _i64)]
+
+
+class HvdHeads(C.Structure):
+    _fields_ = [("p", _vp), ("row_stride", _i64), ("head_stride", _i64)]
 
 
 _SIGNATURES = {
@@ -73,6 +91,13 @@ _SIGNATURES = {
     "hvd_step_host": (_i32, [_vp, C.POINTER(HvdHostStepArgs), _vp]),
     "hvd_verify_commit_noalloc": (_i32, [_i32, _i32, _vp, _i32, _i64, _vp, _i32, _i64] + [_vp] * 13 + [_vp]),
     "hvd_noalloc_last_error": (C.c_char_p, []),
+    "hvd_rope_frequencies": (_i32, [C.POINTER(HvdAttnConfig), C.POINTER(_f64), C.POINTER(_f64)]),
+    "hvd_set_attention": (_i32, [_vp, C.POINTER(HvdAttnConfig)]),
+    "hvd_rope_append": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _vp, _vp, _i32, _i64, _vp, _vp]
+                        + [C.POINTER(HvdHeads)] * 4 + [_vp, _vp]),
+    "hvd_attn_paged": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _vp, _vp, _i32, _i64, _vp, _vp]
+                       + [C.POINTER(HvdHeads)] * 2 + [_vp, _vp, _vp]),
+    "hvd_kv_commit": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _i32, _i64] + [_vp] * 9),
 }
 
 _lib = None
@@ -139,6 +164,53 @@ def hvd_verify_commit_noalloc(B, k_cap, logits, dtype, V, row_off, k_uniform, to
     if st != 0:
         raise HvdError(f"hvd_verify_commit_noalloc: {lib.hvd_status_string(st).decode()}: "
                        f"{lib.hvd_noalloc_last_error().decode()}")
+
+
+class KvCache:
+    """The paged cache of one layer: k, v CUDA tensors [n_pages, page_size, n_kv_heads, head_dim] (a permuted view of
+    [n_pages, n_kv_heads, page_size, head_dim] is as good; the last stride is 1) and the int32 page table [B, pages].
+    Holds the tensors, so that they live as long as it does."""
+
+    def __init__(self, k, v, page_table):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise HvdError("KvCache: k and v are tensors [n_pages, page_size, n_kv_heads, head_dim] of one type, shape and layout")
+        if k.stride(3) != 1 and k.shape[3] > 1:
+            raise HvdError("KvCache: the elements of a head must be contiguous")
+        if page_table.dim() != 2 or not page_table.is_contiguous() or str(page_table.dtype) != "torch.int32":
+            raise HvdError("KvCache: page_table is a contiguous int32 tensor [B, pages]")
+        self.k, self.v, self.page_table = k, v, page_table
+        self._c = HvdKvCache(_ptr(k), _ptr(v), k.shape[0], k.shape[1], page_table.shape[1], _ptr(page_table),
+                             _step(k, 0), _step(k, 1), _step(k, 2))
+
+
+def _step(t, dim):
+    """Stride of a dimension; one of length 1 may carry any, and is given that of whole heads."""
+    return t.stride(dim) if t.shape[dim] > 1 else max(8, t.shape[-1])
+
+
+def _heads(t, what):
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise HvdError(f"{what}: a tensor [rows, heads, head_dim] with contiguous heads is needed")
+    return HvdHeads(_ptr(t), _step(t, 0), _step(t, 1))
+
+
+def make_attn_config(*, n_q_heads, n_kv_heads, head_dim, dtype=BF16, softmax_scale=0.0, rot_dim=None, rot_layout=ROPE_HALVES,
+                     rope_scaling=ROPE_PLAIN, rope_base=10000.0, rope_factor=1.0, rope_original_len=0.0, rope_low=0.0,
+                     rope_high=0.0, rope_magnitude=0.0):
+    """hvd_attn_config; rot_dim defaults to the whole head."""
+    return HvdAttnConfig(n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, head_dim if rot_dim is None else rot_dim,
+                         rot_layout, rope_scaling, rope_base, rope_factor, rope_original_len, rope_low, rope_high, rope_magnitude)
+
+
+def hvd_rope_frequencies(**cfg):
+    """(radians per position of every rotated pair, the factor on cos and sin) of a configuration; no device needed."""
+    c = make_attn_config(**cfg)
+    lib = load_library()
+    freq, mag = (_f64 * max(1, c.rot_dim // 2 if 0 <= c.rot_dim <= 1 << 16 else 1))(), _f64(0.0)
+    st = lib.hvd_rope_frequencies(C.byref(c), freq, C.byref(mag))
+    if st != 0:
+        raise HvdError(f"hvd_rope_frequencies: {lib.hvd_status_string(st).decode()}")
+    return np.array(freq[:c.rot_dim // 2], np.float64), float(mag.value)
 
 
 class Context:
@@ -357,3 +429,47 @@ class Context:
                                _hptr(sel_len), _hptr(accepted), _hptr(committed), _hptr(n_commit),
                                _hptr(status))
         self._check(self._lib.hvd_step_host(self._h, C.byref(args), _stream()), "hvd_step_host")
+
+    def hvd_set_attention(self, **cfg):
+        """Attention geometry and rotary positions of the cache operators (make_attn_config's arguments)."""
+        c = make_attn_config(**cfg)
+        self._check(self._lib.hvd_set_attention(self._h, C.byref(c)), "hvd_set_attention")
+        self.attn = c
+
+    def _cache_arg(self, cache, what):
+        a = getattr(self, "attn", None)
+        if a is not None and (cache.k.shape[2], cache.k.shape[3]) != (a.n_kv_heads, a.head_dim):
+            raise HvdError(f"{what}: the cache has other heads than hvd_set_attention was given")
+        if a is not None and str(cache.k.dtype) != ("torch.float16" if a.dtype == F16 else "torch.bfloat16"):
+            raise HvdError(f"{what}: the cache has another type than hvd_set_attention was given")
+        return C.byref(cache._c)
+
+    def _heads_arg(self, t, heads, total_rows, what):
+        a = getattr(self, "attn", None)
+        if a is not None and (t.dim() != 3 or t.shape[0] < total_rows or t.shape[1] != getattr(a, heads) or t.shape[2] != a.head_dim):
+            raise HvdError(f"{what}: a tensor [total_rows, {heads}, head_dim] is needed")
+        if a is not None and str(t.dtype) != ("torch.float16" if a.dtype == F16 else "torch.bfloat16"):
+            raise HvdError(f"{what}: another type than hvd_set_attention was given")
+        return C.byref(_heads(t, what))
+
+    def hvd_rope_append(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, k, v, q_out, status):
+        w = "hvd_rope_append"
+        h = lambda t, heads: self._heads_arg(t, heads, total_rows, w)
+        self._check(self._lib.hvd_rope_append(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform,
+                                              total_rows, _ptr(sel_len), _ptr(parent), h(q, "n_q_heads"), h(k, "n_kv_heads"),
+                                              h(v, "n_kv_heads"), h(q_out, "n_q_heads"), _ptr(status), _stream()), w)
+
+    def hvd_attn_paged(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, out, lse=None,
+                       status=None):
+        w = "hvd_attn_paged"
+        h = lambda t: self._heads_arg(t, "n_q_heads", total_rows, w)
+        self._check(self._lib.hvd_attn_paged(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform,
+                                             total_rows, _ptr(sel_len), _ptr(parent), h(q), h(out), _ptr(lse), _ptr(status),
+                                             _stream()), w)
+
+    def hvd_kv_commit(self, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
+                      n_commit, new_len):
+        w = "hvd_kv_commit"
+        self._check(self._lib.hvd_kv_commit(self._h, B, self._cache_arg(cache, w), n_layers, layer_stride, _ptr(cache_len),
+                                            _ptr(parent), _ptr(sel_draft), _ptr(sel_len), _ptr(accepted), _ptr(committed),
+                                            _ptr(n_commit), _ptr(new_len), _stream()), w)

@@ -21,6 +21,7 @@ void release(hvd_ctx* c) {
     cudaFree(c->rp_key); cudaFree(c->rp_cnt);
     cudaFree(c->vf_next_unit); cudaFree(c->dev_error); cudaFree(c->vf_row_key); cudaFree(c->vf_alive);
     cudaFree(c->host_ws);
+    cudaFree(c->at_turns); cudaFree(c->at_arrived);
     delete c;
 }
 
@@ -104,9 +105,9 @@ hvd_status hvd_create(hvd_ctx** out, const hvd_config* cfg) {
     c->two_layer = false;
     c->score2_ready = false;
     // programmatic dependent launch of the kernels of a step (bit 0 commit, 1 lookup, 2 stream, 3 one-layer
-    // scoring): the next kernel's CTAs are resident and past their prologue when the previous one ends;
+    // scoring, 4 cache operators): the next kernel's CTAs are resident and past their prologue when the previous one ends;
     // HVD_PDL_MASK=0 turns it off
-    c->pdl_mask = getenv("HVD_PDL_MASK") ? atoi(getenv("HVD_PDL_MASK")) : 15;
+    c->pdl_mask = getenv("HVD_PDL_MASK") ? atoi(getenv("HVD_PDL_MASK")) : 31;
     c->pdl_commit = (c->pdl_mask & 1) != 0;
     c->vf_small_bytes = getenv("HVD_VERIFY_SMALL_BYTES") ? atoll(getenv("HVD_VERIFY_SMALL_BYTES")) : kVerifySmallBytes;
     c->vf_boundary_bytes = getenv("HVD_PREFIX_BOUNDARY_BYTES") ? atoll(getenv("HVD_PREFIX_BOUNDARY_BYTES")) : kPrefixBoundaryBytes;

@@ -102,10 +102,15 @@ struct hvd_ctx {
     long long vf_small_bytes;        // size limit of the warp-per-batch kernels (HVD_VERIFY_SMALL_BYTES; 0 = never)
     long long vf_boundary_bytes;     // prefix verification: streamed bytes that one window boundary is worth (HVD_PREFIX_BOUNDARY_BYTES)
     // device staging of the host-buffer entry point (grown on demand)
-    int pdl_mask;     // ... for the three kernels of a step: bit 0 commit, 1 lookup, 2 stream, 3 one-layer scoring (default all)
+    int pdl_mask;     // ... for the kernels of a step: bit 0 commit, 1 lookup, 2 stream, 3 one-layer scoring, 4 cache operators (default all)
     bool pdl_commit;  // bit 0 of the mask
     char* host_ws;
     size_t host_ws_bytes;
+    // cache operators (hvd_set_attention)
+    hvd_attn_config attn;            // with the defaults filled in
+    bool has_attention;
+    unsigned long long* at_turns;    // [HVD_MAX_HEAD_DIM / 2] angular frequencies in 2^-64 turns per position
+    uint32_t* at_arrived;            // [max_batch] zero at rest: CTAs of a request that have read its length
     char last_error[256];
 };
 

@@ -1,0 +1,123 @@
+// hvd_kv_commit: after a verification, the accepted nodes of a token tree move behind the cached tokens, in every layer.
+//
+// The accepted path ascends (a child has a larger index than its parent), so the j-th accepted node never lies before
+// slot j: a thread that owns one 16-byte column of the cache rows may read any later source before it writes an
+// earlier target, and the moves of a request need no copy aside.  Bound by the bytes moved and by the two or three dependent
+// global round trips at the start (lengths, tree, page table).
+#include "hvd_attn.cuh"
+
+namespace hvd {
+
+namespace {
+
+constexpr int kKvThreads = 256;
+constexpr uint32_t kFull = 0xffffffffu;
+
+__global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArgs a) {
+    __shared__ int64_t from[kTreeRows], to[kTreeRows];
+    __shared__ int n_moves;
+    const ChunkArgs& c = a.c;
+    const int b = blockIdx.x;
+    pdl_trigger();
+    pdl_wait();
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        const int base = c.cache_len[b];
+        const int w = a.n_commit[b];
+        const bool usable = w > 0 && base >= 0 && (int64_t)base + w <= (int64_t)c.table_stride * c.page_size;
+        if (lane == 0) {
+            // new_len may be cache_len: it is written once every CTA of the request has read the old length
+            __threadfence();
+            const uint32_t n = atomicAdd(&a.arrived[b], 1u);
+            if (n + 1 == gridDim.y) {
+                a.arrived[b] = 0u;  // zero at rest
+                a.new_len[b] = usable ? base + w : base;
+            }
+        }
+        int moves = 0;
+        if (usable && c.parent) {
+            const int kc = c.k_cap;
+            const int m = max(0, min(c.sel_len[b], kc));
+            const int most = min(min(a.accepted[b], w - 1), m);
+            const int32_t* z = a.committed + (int64_t)b * (kc + 1);
+            int dt[2], pr[2], zt[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {  // nodes lane, lane + 32
+                const int i = lane + 32 * k;
+                dt[k] = i < m ? a.sel_draft[(int64_t)b * kc + i] : -1;
+                pr[k] = i < m ? c.parent[(int64_t)b * kc + i] : -2;
+                zt[k] = i < kc ? z[i] : -1;
+            }
+            int cur = -1;
+            int src[2] = {-1, -1};  // lane holds the nodes of steps lane, lane + 32
+            int steps = 0;
+            for (; steps < most; ++steps) {
+                const int want = __shfl_sync(kFull, steps < 32 ? zt[0] : zt[1], steps & 31);
+                const uint32_t b0 = __ballot_sync(kFull, lane < m && lane > cur && pr[0] == cur && dt[0] == want);
+                const uint32_t b1 = __ballot_sync(kFull, lane + 32 < m && lane + 32 > cur && pr[1] == cur && dt[1] == want);
+                if ((b0 | b1) == 0u) break;
+                cur = b0 ? __ffs(b0) - 1 : 32 + __ffs(b1) - 1;
+                if ((steps & 31) == lane) src[steps >> 5] = cur;
+            }
+            // page and slot of every move; a move that stays in place is left out, a bad page ends the list
+            bool bad[2];
+            int64_t fo[2] = {0, 0}, ta[2] = {0, 0};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int j = lane + 32 * k;
+                bad[k] = false;
+                if (j < steps) {
+                    const int sf = base + 1 + src[k], st = base + 1 + j;
+                    const bool inside = (int64_t)base + 1 + src[k] < (int64_t)c.table_stride * c.page_size;
+                    const int64_t pf = inside ? page_of(c, b, sf) : -1, pt = page_of(c, b, st);
+                    bad[k] = pf < 0 || pt < 0;
+                    if (!bad[k]) { fo[k] = slot_offset(c, pf, sf); ta[k] = slot_offset(c, pt, st); }
+                }
+            }
+            const uint32_t f0 = __ballot_sync(kFull, bad[0]), f1 = __ballot_sync(kFull, bad[1]);
+            const int end = f0 ? __ffs(f0) - 1 : (f1 ? 32 + __ffs(f1) - 1 : steps);
+            const uint32_t m0 = __ballot_sync(kFull, lane < end && src[0] != lane);
+            const uint32_t m1 = __ballot_sync(kFull, lane + 32 < end && src[1] != lane + 32);
+            const uint32_t below = (1u << lane) - 1u;
+            if ((m0 >> lane) & 1u) { const int s = __popc(m0 & below); from[s] = fo[0]; to[s] = ta[0]; }
+            if ((m1 >> lane) & 1u) { const int s = __popc(m0) + __popc(m1 & below); from[s] = fo[1]; to[s] = ta[1]; }
+            moves = __popc(m0) + __popc(m1);
+        }
+        if (lane == 0) n_moves = moves;
+    }
+    __syncthreads();
+    const int n = n_moves;
+    if (n == 0) return;
+    const int nvec = a.head_dim / 8, heads = a.n_kv_heads;
+    const int64_t total = (int64_t)a.n_layers * 2 * heads * nvec;
+    for (int64_t w = (int64_t)blockIdx.y * kKvThreads + threadIdx.x; w < total; w += (int64_t)gridDim.y * kKvThreads) {
+        const int e = (int)(w % nvec);
+        const int64_t r = w / nvec;
+        const int h = (int)(r % heads);
+        const int64_t l2 = r / heads;  // layer * 2 + (key or value)
+        char* pool = (l2 & 1) ? c.v : c.k;
+        const int64_t col = (l2 >> 1) * a.layer_stride + (int64_t)h * c.head_stride + 8 * e;
+        for (int j = 0; j < n; j += 8) {
+            uint4 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (j + i < n) x[i] = *reinterpret_cast<const uint4*>(pool + 2 * (col + from[j + i]));
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (j + i < n) *reinterpret_cast<uint4*>(pool + 2 * (col + to[j + i])) = x[i];
+        }
+    }
+}
+
+}  // namespace
+
+hvd_status launch_kv_commit(hvd_ctx* ctx, const KvCommitArgs& a, cudaStream_t stream) {
+    const int64_t vecs = (int64_t)a.n_layers * 2 * a.n_kv_heads * (a.head_dim / 8);
+    int64_t gy = a.c.parent ? (vecs + kKvThreads - 1) / kKvThreads : 1;
+    if (gy > 1024) gy = 1024;
+    const cudaError_t e = launch_kernel((ctx->pdl_mask & 16) != 0, kv_commit_kernel, dim3((unsigned)a.c.B, (unsigned)gy),
+                                        dim3(kKvThreads), 0, stream, a);
+    return e == cudaSuccess ? HVD_OK : cuda_fail(ctx, e, "kv_commit_kernel");
+}
+
+}  // namespace hvd

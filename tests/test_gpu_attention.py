@@ -1,0 +1,290 @@
+"""hvd_attn_paged against softmax attention in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests import attn_reference as R
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+def run(p, ctx=None, lse=True, q=None, out=None, row_off=True, cache=None, **cfg):
+    p.device()
+    own = ctx is None
+    ctx = ctx or p.context(**cfg)
+    q = p.q if q is None else q
+    out = torch.full((p.total, p.hq, p.d), float("nan"), dtype=p.dtype, device="cuda") if out is None else out
+    ls = torch.full((p.total, p.hq), float("nan"), device="cuda") if lse else None
+    ctx.hvd_attn_paged(p.B, cache or p.cache(), p.t_len, p.t_off if row_off else None, p.k_uniform, p.total, p.t_sel, p.t_par, q,
+                       out, ls, p.status)
+    torch.cuda.synchronize()
+    assert ctx.hvd_device_status() == 0
+    if own:
+        ctx.close()
+    return out, ls
+
+
+def check(p, scale=None, **kw):
+    p.fill()
+    out, lse = run(p, **({} if scale is None else dict(softmax_scale=scale)), **kw)
+    R.check_attention(p, out, lse, R.attention(p, scale))
+    assert (p.status == 0).all()
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d", [8, 16, 64, 72, 80, 96, 120, 128])
+def test_head_dims(d, dtype):
+    check(R.Problem(lens=[0, 1, 127, 300], rows=[3, 1, 9, 5], hq=8, hkv=2, d=d, page=16, dtype=dtype, seed=d))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (3, 1), (10, 2), (12, 4), (7, 1), (32, 4), (128, 1), (33, 3)])
+def test_head_groups(hq, hkv):
+    check(R.Problem(lens=[5, 140, 260], rows=[1, 17, 40], hq=hq, hkv=hkv, d=64, page=32, seed=hq))
+
+
+@pytest.mark.parametrize("page", [8, 16, 24, 40, 48, 64, 128, 136, 256, 1024])
+@pytest.mark.parametrize("order", ["slots", "heads"])
+def test_page_sizes(page, order):
+    check(R.Problem(lens=[1, 7, 129, 383, 700], rows=[2, 9, 1, 17, 4], hq=4, hkv=2, d=128, page=page, order=order, seed=page))
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 7, 8, 31, 62, 63, 64, 126, 127, 128, 129, 254, 255, 256, 257, 383, 511, 1000, 2049])
+def test_lengths_around_the_tile(n):
+    check(R.Problem(lens=[n, n + 1], rows=[1, 2], hq=4, hkv=1, d=128, page=16, seed=n))
+
+
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 385, 600])
+@pytest.mark.parametrize("hq", [1, 4])
+def test_chunk_lengths(rows, hq):
+    """One to several tiles of query rows; the causal edge inside and on the border of key tiles."""
+    check(R.Problem(lens=[0, 100], rows=[rows, rows], hq=hq, hkv=1, d=64, page=16, seed=rows))
+
+
+def test_rows_from_k_uniform_and_ragged_selection():
+    p = R.Problem(lens=[40, 0, 333, 129], rows=[17] * 4, sel=[16, 0, 5, 99], k_cap=16, hq=8, hkv=2, d=128, page=16, uniform=True)
+    out, lse = check(p, row_off=False)
+    for b, m in enumerate(p.n_new):                            # rows that are no new token
+        r = slice(int(p.off[b]) + m, int(p.off[b + 1]))
+        assert (out[r] == 0).all() and torch.isinf(lse[r]).all()
+
+
+def test_empty_requests_and_an_empty_batch():
+    check(R.Problem(lens=[10, 0, 50, 3], rows=[0, 0, 4, 0], hq=4, hkv=2, d=64, page=16))
+    p = R.Problem(lens=[10, 0], rows=[0, 0], hq=4, hkv=2, d=64, page=16)
+    check(p)
+
+
+@pytest.mark.parametrize("nodes,hq,hkv,dtype", [(1, 4, 1, BF), (32, 8, 2, BF), (64, 16, 2, HF), (64, 4, 4, BF), (33, 24, 3, BF)])
+def test_trees(nodes, hq, hkv, dtype):
+    rng = np.random.default_rng(nodes)
+    B = 6
+    sel = [nodes, max(0, nodes - 1), 0, nodes // 2, nodes, nodes]
+    check(R.Problem(lens=[0, 1, 200, 255, 127, int(rng.integers(0, 900))], rows=[nodes + 1] * B, sel=sel, hq=hq, hkv=hkv, d=64,
+                    page=16, dtype=dtype, tree=True, seed=nodes))
+
+
+def test_unreachable_nodes_see_nothing():
+    p = R.Problem(lens=[100, 30, 0], rows=[33] * 3, sel=[32] * 3, hq=4, hkv=1, d=64, page=16, tree=True, bad=0.2, seed=5)
+    out, lse = check(p)
+    lost = [int(p.off[b]) + i for b in range(3) for i in range(33) if R.line_of(p.parent[b], i) is None]
+    assert len(lost) > 5 and (out[lost] == 0).all() and torch.isinf(lse[lost]).all()
+
+
+def test_a_chain_as_a_tree_gives_the_chain():
+    kw = dict(lens=[77, 128, 0], rows=[20, 9, 33], sel=[19, 8, 32], hq=8, hkv=2, d=128, page=16, seed=3)
+    a, b = R.Problem(**kw), R.Problem(**kw)
+    b.parent = np.tile(np.arange(-1, 63, dtype=np.int32), (3, 1))
+    for x, y in zip(check(a), check(b)):
+        assert torch.equal(x, y)
+
+
+def test_strided_rows():
+    """q a slice of a fused projection, out inside a wider array."""
+    p = R.Problem(lens=[50, 300], rows=[9, 17], hq=8, hkv=2, d=64, page=16, seed=9)
+    wide = torch.full((p.total, p.hq + 4, 80), float("nan"), dtype=BF, device="cuda")
+    wide[:, 2:10, 8:72] = p.q
+    room = torch.full((p.total, 3, p.hq, 72), 7.0, dtype=BF, device="cuda")
+    out = room[:, 1, :, :64]
+    check(p, q=wide[:, 2:10, 8:72], out=out)
+    assert (room[:, 0] == 7).all() and (room[:, 2] == 7).all() and (room[:, 1, :, 64:] == 7).all()
+
+
+@pytest.mark.parametrize("scale", [0.01, 0.5, 3.0])
+def test_softmax_scale(scale):
+    check(R.Problem(lens=[400, 90], rows=[5, 40], hq=4, hkv=2, d=64, page=16, seed=1, sharp=1.0), scale=scale)
+
+
+def test_maxima_that_climb_and_fall():
+    """Scores that rise by hundreds along the keys, stay far below zero, or are all equal."""
+    p = R.Problem(lens=[1500, 1500, 1500, 600], rows=[9, 9, 9, 70], hq=4, hkv=1, d=64, page=16, seed=2)
+    one = torch.ones(64, device="cuda")
+    p.q = torch.ones_like(p.q)
+    for b, f in enumerate([lambda n: torch.linspace(-60, 60, n), lambda n: torch.linspace(60, -60, n), lambda n: torch.full((n,), -90.0),
+                           lambda n: torch.linspace(-20, 20, n)]):
+        p.kd[b] = (f(p.kd[b].shape[0]).cuda()[:, None, None] * one / 8).to(BF).expand_as(p.kd[b]).contiguous()
+    check(p)
+
+
+def test_slots_behind_the_chunk_may_hold_anything():
+    for fill in (float("nan"), float("inf"), -float("inf"), 3.0e38):
+        p = R.Problem(lens=[100, 37, 127, 0], rows=[3, 1, 1, 1], hq=4, hkv=2, d=128, page=64, seed=4)
+        p.k.fill_(fill)
+        p.v.fill_(fill)
+        check(p)
+
+
+def test_unusable_requests_are_skipped():
+    p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
+    want = R.attention(p)
+    p.device()
+    ctx = p.context()
+    lens = p.t_len.clone()
+    lens[1], lens[3] = -1, p.table.shape[1] * 16 - 2           # one row too many for the table
+    out, lse = torch.full_like(p.q, 5.0), torch.full((p.total, p.hq), 5.0, device="cuda")
+    ctx.hvd_attn_paged(p.B, p.cache(), lens, p.t_off, 0, p.total, p.t_sel, None, p.q, out, lse, p.status)
+    assert p.status.tolist() == [0, 2, 0, 2, 0]
+    for b in (1, 3):
+        r = slice(int(p.off[b]), int(p.off[b + 1]))
+        assert (out[r] == 0).all() and torch.isinf(lse[r]).all()
+        want[0][r], want[1][r], want[2][r] = 0, -np.inf, 0
+    R.check_attention(p, out, lse, want)
+    # rows outside the arrays, rows that run backwards
+    off = p.t_off.clone()
+    off[2], off[5] = 1000, -7
+    ctx.hvd_attn_paged(p.B, p.cache(), p.t_len, off, 0, p.total, p.t_sel, None, p.q, out, lse, p.status)
+    assert p.status.tolist() == [0, 2, 2, 0, 2]
+    assert ctx.hvd_device_status() == 0
+    ctx.close()
+
+
+def test_page_entries_outside_the_pool_stand_for_zeros():
+    p = R.Problem(lens=[100, 60], rows=[3, 2], hq=4, hkv=2, d=64, page=16, seed=7).fill()
+    kd, vd = [x.clone() for x in p.kd], [x.clone() for x in p.vd]
+    for b, j, v in ((0, 2, -1), (0, 4, p.n_pages), (1, 0, 2 ** 31 - 1)):
+        p.table[b, j] = v
+        kd[b][16 * j:16 * j + 16] = 0
+        vd[b][16 * j:16 * j + 16] = 0
+    out, lse = run(p)
+    R.check_attention(p, out, lse, R.attention(p, kd=kd, vd=vd))
+
+
+def test_long_ragged_batch_split_over_the_sms():
+    """Contexts from one token to 40 000: most are cut into pieces that are joined again."""
+    rng = np.random.default_rng(8)
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(20000), 24))] + [40001]
+    check(R.Problem(lens=lens, rows=[int(x) for x in rng.integers(1, 18, 25)], hq=8, hkv=2, d=64, page=16, seed=8))
+
+
+@pytest.mark.parametrize("lens,rows,hq,hkv,d", [([30000], [1], 32, 8, 128), ([9001], [65], 16, 2, 128), ([50], [700], 16, 2, 128),
+                                                ([12345, 3], [64, 300], 8, 1, 128)])
+def test_few_requests(lens, rows, hq, hkv, d):
+    check(R.Problem(lens=lens, rows=rows, hq=hq, hkv=hkv, d=d, page=32, seed=11))
+
+
+def test_results_do_not_depend_on_the_run():
+    p = R.Problem(lens=[5000, 130, 2222], rows=[9, 17, 1], hq=8, hkv=2, d=128, page=16, seed=12).fill()
+    p.device()
+    ctx = p.context()
+    first = None
+    for _ in range(4):
+        out, lse = run(p, ctx=ctx)
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    ctx.close()
+
+
+def test_another_stream_and_a_graph():
+    p = R.Problem(lens=[700, 1300], rows=[9, 9], hq=8, hkv=2, d=128, page=16, seed=13).fill()
+    want = R.attention(p)
+    p.device()
+    ctx, cache, out, lse = p.context(), p.cache(), torch.zeros_like(p.q), torch.zeros(p.total, p.hq, device="cuda")
+    call = lambda: ctx.hvd_attn_paged(p.B, cache, p.t_len, p.t_off, 0, p.total, None, None, p.q, out, lse, p.status)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+    s.synchronize()
+    R.check_attention(p, out, lse, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    out.zero_(), lse.zero_()
+    g.replay(), g.replay()
+    torch.cuda.synchronize()
+    R.check_attention(p, out, lse, want)
+    del g
+    ctx.close()
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 2^32 bytes and 2^31 elements per array; the request's pages lie at its end."""
+    p = R.Problem(lens=[500], rows=[5], hq=4, hkv=2, d=128, page=64, seed=14, pool_pages=(1 << 31) // (64 * 256) + 64)
+    p.table[0, :8] = p.n_pages - 1 - np.arange(8)
+    check(p)
+
+
+def test_lse_and_status_are_optional():
+    p = R.Problem(lens=[90], rows=[4], hq=4, hkv=2, d=64, page=16, seed=15).fill().device()
+    ctx, out = p.context(), torch.zeros_like(p.q)
+    ctx.hvd_attn_paged(1, p.cache(), p.t_len, p.t_off, 0, p.total, None, None, p.q, out)
+    R.check_attention(p, out, None, R.attention(p))
+    ctx.close()
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_batches(seed):
+    rng = np.random.default_rng(1000 + seed)
+    B = int(rng.integers(1, 12))
+    tree = bool(rng.random() < 0.4)
+    hkv = int(rng.integers(1, 5))
+    g = int(rng.choice([1, 2, 3, 4, 5, 8, 16]))
+    most = 40 if rng.random() < 0.7 else 300
+    rows = [int(x) for x in rng.integers(1, (66 if tree else most) + 1, B)]
+    sel = [int(rng.integers(-1, r + 3)) for r in rows] if tree or rng.random() < 0.5 else None
+    if sel is not None:
+        rows = [min(r, 65) for r in rows]
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(6000), B)) - 1]
+    check(R.Problem(lens=lens, rows=rows, sel=sel, hq=g * hkv, hkv=hkv, d=int(rng.choice([32, 64, 80, 128, 128])),
+                    page=int(rng.choice([8, 16, 32, 56, 64, 256])), dtype=BF if rng.random() < 0.7 else HF, tree=True if tree else None,
+                    bad=0.05, order=str(rng.choice(["slots", "heads"])), seed=seed))
+
+
+def test_refusals():
+    import paper_2606_01019_b200 as H
+    p = R.Problem(lens=[20], rows=[4], hq=4, hkv=2, d=64, page=16).fill().device()
+    plain = H.Context(max_batch=1, k_cap=4, max_hist_len=16, max_rows=4, max_vocab=8)
+    out, lse = torch.zeros_like(p.q), torch.zeros(p.total, p.hq, device="cuda")
+    args = lambda **o: [o.get("B", 1), o.get("cache") or p.cache(), p.t_len, p.t_off, 0, o.get("rows", p.total), o.get("sel"), o.get("par"),
+                        o.get("q", p.q), o.get("out", out), lse, p.status]
+
+    def refused(ctx, text, **o):
+        with pytest.raises(H.HvdError, match=text):
+            ctx.hvd_attn_paged(*args(**o))
+    refused(plain, "hvd_set_attention first")
+    plain.close()
+    ctx = p.context()
+    refused(ctx, "B outside", B=0)
+    refused(ctx, "B outside", B=2)
+    refused(ctx, "parent needs sel_len", par=torch.zeros(1, 64, dtype=torch.int32, device="cuda"))
+    refused(ctx, "another array", out=p.q)
+    refused(ctx, "total_rows", rows=p.total + 1, q=torch.zeros(9, 4, 64, dtype=BF, device="cuda"), out=torch.zeros(9, 4, 64, dtype=BF, device="cuda"))
+    refused(ctx, "16-byte aligned", q=torch.zeros(4 * 256 + 4, dtype=BF, device="cuda")[4:].reshape(4, 4, 64))
+    refused(ctx, "multiples of 8", q=torch.zeros(4, 4, 68, dtype=BF, device="cuda")[..., :64])
+    refused(ctx, "another type", q=p.q.half())
+    refused(ctx, "n_q_heads", q=torch.zeros(4, 8, 64, dtype=BF, device="cuda"))
+    odd = torch.zeros(4, 12, 2, 64, dtype=BF, device="cuda")
+    refused(ctx, "page_size", cache=H.KvCache(odd, odd.clone(), p.t_table))
+    for bad in (dict(head_dim=136), dict(head_dim=60), dict(n_q_heads=5), dict(n_q_heads=0), dict(dtype=H.F32), dict(rot_dim=3),
+                dict(rot_dim=66), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(rope_base=1.0), dict(rot_layout=2),
+                dict(rope_scaling=9), dict(rope_scaling=H.ROPE_LINEAR, rope_factor=0.5), dict(rope_scaling=H.ROPE_PARTS, rope_factor=2.0),
+                dict(n_q_heads=258, n_kv_heads=2)):
+        with pytest.raises(H.HvdError, match="hvd_set_attention"):
+            p.context(**bad)
+    # what was set stays usable after a refusal, and a new geometry takes the old one's place
+    with pytest.raises(H.HvdError):
+        ctx.hvd_set_attention(n_q_heads=4, n_kv_heads=3, head_dim=64)
+    ctx.hvd_attn_paged(*args())
+    R.check_attention(p, out, lse, R.attention(p))
+    ctx.close()
