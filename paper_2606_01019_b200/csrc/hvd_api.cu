@@ -21,7 +21,7 @@ void release(hvd_ctx* c) {
     cudaFree(c->rp_key); cudaFree(c->rp_cnt);
     cudaFree(c->vf_next_unit); cudaFree(c->dev_error); cudaFree(c->vf_row_key); cudaFree(c->vf_alive);
     cudaFree(c->host_ws);
-    cudaFree(c->at_turns); cudaFree(c->at_arrived);
+    cudaFree(c->at_turns); cudaFree(c->at_arrived); cudaFree(c->at_ws);
     delete c;
 }
 

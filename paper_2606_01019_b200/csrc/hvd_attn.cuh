@@ -130,6 +130,8 @@ struct KvCommitArgs {
 };
 
 hvd_status launch_rope_append(hvd_ctx* ctx, const RopeArgs& a, bool f16, int layout, cudaStream_t stream);
+size_t attn_workspace_bytes(int num_sms, int head_dim);
+hvd_status attn_setup(hvd_ctx* ctx);  // per-device opt-ins of the attention kernels
 hvd_status launch_attn(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream);
 hvd_status launch_kv_commit(hvd_ctx* ctx, const KvCommitArgs& a, cudaStream_t stream);
 
