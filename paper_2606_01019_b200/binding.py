@@ -179,19 +179,15 @@ class KvCache:
         if page_table.dim() != 2 or not page_table.is_contiguous() or str(page_table.dtype) != "torch.int32":
             raise HvdError("KvCache: page_table is a contiguous int32 tensor [B, pages]")
         self.k, self.v, self.page_table = k, v, page_table
+        self.heads, self.type = (k.shape[2], k.shape[3]), k.dtype
         self._c = HvdKvCache(_ptr(k), _ptr(v), k.shape[0], k.shape[1], page_table.shape[1], _ptr(page_table),
                              _step(k, 0), _step(k, 1), _step(k, 2))
+        self._ref = C.byref(self._c)
 
 
 def _step(t, dim):
     """Stride of a dimension; one of length 1 may carry any, and is given that of whole heads."""
     return t.stride(dim) if t.shape[dim] > 1 else max(8, t.shape[-1])
-
-
-def _heads(t, what):
-    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise HvdError(f"{what}: a tensor [rows, heads, head_dim] with contiguous heads is needed")
-    return HvdHeads(_ptr(t), _step(t, 0), _step(t, 1))
 
 
 def make_attn_config(*, n_q_heads, n_kv_heads, head_dim, dtype=BF16, softmax_scale=0.0, rot_dim=None, rot_layout=ROPE_HALVES,
@@ -230,6 +226,7 @@ class Context:
             raise HvdError(f"hvd_create: {self._lib.hvd_status_string(st).decode()}")
         self.k_cap = k_cap
         self.hidden = hidden
+        self.attn = None
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -432,44 +429,75 @@ class Context:
 
     def hvd_set_attention(self, **cfg):
         """Attention geometry and rotary positions of the cache operators (make_attn_config's arguments)."""
+        import torch
         c = make_attn_config(**cfg)
         self._check(self._lib.hvd_set_attention(self._h, C.byref(c)), "hvd_set_attention")
         self.attn = c
+        # the current stream's handle without a Stream object: these calls are made once per layer
+        self._raw_stream, self._dev = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device()
+        self._attn_type = torch.float16 if c.dtype == F16 else torch.bfloat16
+        # the calls' argument structs, filled anew by every call (the library reads them before it returns)
+        self._arg = [HvdHeads() for _ in range(4)]
+        self._arg_ref = [C.byref(h) for h in self._arg]
 
     def _cache_arg(self, cache, what):
-        a = getattr(self, "attn", None)
-        if a is not None and (cache.k.shape[2], cache.k.shape[3]) != (a.n_kv_heads, a.head_dim):
-            raise HvdError(f"{what}: the cache has other heads than hvd_set_attention was given")
-        if a is not None and str(cache.k.dtype) != ("torch.float16" if a.dtype == F16 else "torch.bfloat16"):
-            raise HvdError(f"{what}: the cache has another type than hvd_set_attention was given")
-        return C.byref(cache._c)
+        a = self.attn
+        if a is not None:
+            if cache.heads != (a.n_kv_heads, a.head_dim):
+                raise HvdError(f"{what}: the cache has other heads than hvd_set_attention was given")
+            if cache.type is not self._attn_type:
+                raise HvdError(f"{what}: the cache has another type than hvd_set_attention was given")
+        return cache._ref
 
-    def _heads_arg(self, t, heads, total_rows, what):
-        a = getattr(self, "attn", None)
-        if a is not None and (t.dim() != 3 or t.shape[0] < total_rows or t.shape[1] != getattr(a, heads) or t.shape[2] != a.head_dim):
-            raise HvdError(f"{what}: a tensor [total_rows, {heads}, head_dim] is needed")
-        if a is not None and str(t.dtype) != ("torch.float16" if a.dtype == F16 else "torch.bfloat16"):
+    def _heads_arg(self, i, t, heads, total_rows, what):
+        """Argument struct i for rows of heads: a tensor [total_rows or more, heads, head_dim] with contiguous heads."""
+        a = self.attn
+        if a is None:
+            return None      # the library says what is missing
+        shape = t.shape
+        if len(shape) != 3 or shape[0] < total_rows or shape[1] != heads or shape[2] != a.head_dim:
+            raise HvdError(f"{what}: a tensor [total_rows, {heads}, {a.head_dim}] (rows, n_q_heads or n_kv_heads, head_dim) is needed")
+        if t.dtype is not self._attn_type:
             raise HvdError(f"{what}: another type than hvd_set_attention was given")
-        return C.byref(_heads(t, what))
+        row, head, e = t.stride()
+        if e != 1:
+            raise HvdError(f"{what}: the elements of a head must be contiguous")
+        h = self._arg[i]
+        h.p = t.data_ptr()
+        # a dimension of length 1 may carry any stride
+        h.row_stride = row if shape[0] > 1 else shape[1] * a.head_dim
+        h.head_stride = head if shape[1] > 1 else a.head_dim
+        return self._arg_ref[i]
+
+    def _head_counts(self):
+        a = self.attn
+        return (0, 0) if a is None else (a.n_q_heads, a.n_kv_heads)
 
     def hvd_rope_append(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, k, v, q_out, status):
         w = "hvd_rope_append"
-        h = lambda t, heads: self._heads_arg(t, heads, total_rows, w)
-        self._check(self._lib.hvd_rope_append(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform,
-                                              total_rows, _ptr(sel_len), _ptr(parent), h(q, "n_q_heads"), h(k, "n_kv_heads"),
-                                              h(v, "n_kv_heads"), h(q_out, "n_q_heads"), _ptr(status), _stream()), w)
+        nq, nkv = self._head_counts()
+        h = self._heads_arg
+        st = self._lib.hvd_rope_append(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform, total_rows,
+                                       _ptr(sel_len), _ptr(parent), h(0, q, nq, total_rows, w), h(1, k, nkv, total_rows, w),
+                                       h(2, v, nkv, total_rows, w), h(3, q_out, nq, total_rows, w), _ptr(status), self._raw_stream(self._dev) if self.attn is not None else None)
+        if st:
+            self._check(st, w)
 
     def hvd_attn_paged(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, out, lse=None,
                        status=None):
         w = "hvd_attn_paged"
-        h = lambda t: self._heads_arg(t, "n_q_heads", total_rows, w)
-        self._check(self._lib.hvd_attn_paged(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform,
-                                             total_rows, _ptr(sel_len), _ptr(parent), h(q), h(out), _ptr(lse), _ptr(status),
-                                             _stream()), w)
+        nq, _ = self._head_counts()
+        st = self._lib.hvd_attn_paged(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform, total_rows,
+                                      _ptr(sel_len), _ptr(parent), self._heads_arg(0, q, nq, total_rows, w),
+                                      self._heads_arg(1, out, nq, total_rows, w), _ptr(lse), _ptr(status), self._raw_stream(self._dev) if self.attn is not None else None)
+        if st:
+            self._check(st, w)
 
     def hvd_kv_commit(self, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
                       n_commit, new_len):
         w = "hvd_kv_commit"
-        self._check(self._lib.hvd_kv_commit(self._h, B, self._cache_arg(cache, w), n_layers, layer_stride, _ptr(cache_len),
-                                            _ptr(parent), _ptr(sel_draft), _ptr(sel_len), _ptr(accepted), _ptr(committed),
-                                            _ptr(n_commit), _ptr(new_len), _stream()), w)
+        st = self._lib.hvd_kv_commit(self._h, B, self._cache_arg(cache, w), n_layers, layer_stride, _ptr(cache_len),
+                                     _ptr(parent), _ptr(sel_draft), _ptr(sel_len), _ptr(accepted), _ptr(committed),
+                                     _ptr(n_commit), _ptr(new_len), self._raw_stream(self._dev) if self.attn is not None else None)
+        if st:
+            self._check(st, w)

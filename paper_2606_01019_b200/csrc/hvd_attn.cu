@@ -1,15 +1,18 @@
 // hvd_attn_paged: attention of a chunk's rows over the paged cache, on the 5th-generation tensor cores.
 //
 // The rows of a key/value head are the chunk's tokens times the query heads of its group, packed into tiles of
-// 128 rows; keys come in tiles of 128.  Per pair of tiles, S = Q K^T lands in tensor memory, a warpgroup turns it into
+// 128 rows; keys come in tiles of 64.  Per pair of tiles, S = Q K^T lands in tensor memory, a warpgroup turns it into
 // weights P = exp2(S - m) with the running maximum m and sum of a softmax (one thread per row: no shuffles), and
 // O += P V takes P from tensor memory.
 //
-// Two STREAMS of such products run against each other, so that one's softmax hides behind the other's products:
+// Two STREAMS of such steps run against each other, each with two score buffers, so that products run ahead of the
+// softmax:
 //   wide items (more than 128 rows)   the streams are two row tiles that share every key tile
 //   narrow items                      the streams are the even and the odd key tiles of one row tile, joined at the end
-// Roles of the 12 warps: 0-3 and 4-7 softmax, rescaling and output of stream 0 and 1; 8 issues the products; 9 the
-// TMA loads, box by box through the page table; 10 and 11 only lend their registers.  K and V tiles share one ring of slots in the order of their use.
+// Tensor memory, 512 columns: scores [stream][buffer][64] (the weights overwrite the scores they come from), sums [stream][128].
+// Roles of the 12 warps: 0-3 and 4-7 softmax, rescaling and output of stream 0 and 1; 8 issues the products; 9 deals out the
+// work and loads queries and keys, 10 the values, box by box through the page table, by TMA into a ring of slots each;
+// 11 only lends its registers.
 //
 // Work is counted in key tiles over all (request, head, group of rows) items and dealt to the SMs in equal
 // consecutive shares, whatever the lengths; every CTA finds its share from the lengths itself.  An item that
@@ -28,28 +31,42 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9, kLoadVWarp = 10;
 constexpr int kThreads = 384;
 // registers: 384 threads start with 168 each; the softmax warpgroups take 208, the third keeps 88 (208 + 208 + 88 = 3 * 168)
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 constexpr int kFinishThreads = 256;
 constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value (weights up to 2^8 are exact in either type)
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kPieces = 4;             // pieces of work announced ahead
 
 template <int DP> struct Shape {
-    static constexpr int kHalves = DP / 64;                     // 128-byte columns of a tile row
-    static constexpr int kHalfBytes = 128 * 128;
-    static constexpr int kTileBytes = kHalves * kHalfBytes;     // one tile of Q, K or V
-    static constexpr int kSlots = DP == 128 ? 5 : 8;            // K / V ring: 160 or 128 KB
+    static constexpr int kHalves = DP / 64;                         // 128-byte columns of a tile row
+    static constexpr int kQHalf = kTileRows * 128, kQBytes = kHalves * kQHalf;
+    static constexpr int kKvHalf = kTileKeys * 128, kKvBytes = kHalves * kKvHalf;
+    static constexpr int kKSlots = DP == 128 ? 5 : 9, kVSlots = DP == 128 ? 5 : 10;  // the rings: 160 or 152 KB
+    static constexpr int kSlots = kKSlots + kVSlots;
+};
+constexpr int kMaxSlots = 20;
+
+struct Piece {  // what a CTA does of one item
+    int b, h, qt;
+    int r0, base;       // the request's first row, tokens cached before the chunk
+    int tok0, n_tok;    // tokens of the item; n_tok = 0: no more work
+    int kv0, kv1, nkv;  // key tiles of the piece, of the item
+    int c_last;         // the CTA that holds the item's last tile
+    int pad;
 };
 
 struct Shared {  // behind the tiles
-    uint64_t full[8], empty[8];      // ring slots
-    uint64_t q_full, q_empty;        // the item's query tiles
-    uint64_t s_full[2], p_full[2];   // scores written, weights written
-    uint64_t o_full[2];              // a step's product with V is done
-    uint64_t stats, o_free;          // maxima and sums of both streams exchanged; the item's sums are read
+    uint64_t full[kMaxSlots], empty[kMaxSlots];  // slots of the K ring, then of the V ring
+    uint64_t q_full, q_empty;                    // the item's query tiles
+    uint64_t s_full[2][2], p_full[2][2];         // [stream][buffer] scores written, weights written
+    uint64_t o_full[2][2];                       // [stream][buffer] a step's product with V is done
+    uint64_t stats, o_free;                      // maxima and sums of both streams exchanged; the item's sums are read
+    uint64_t piece_full[kPieces], piece_empty[kPieces];
     uint64_t drain;
+    Piece piece[kPieces];
     uint32_t tmem;
     int gave_up;
     int start_b;
@@ -57,12 +74,13 @@ struct Shared {  // behind the tiles
     long long warp_sum[kThreads / 32];
     float m[2][128], l[2][128];  // [stream][row]
 };
-template <int DP> constexpr int kSmemBytes = (2 + Shape<DP>::kSlots) * Shape<DP>::kTileBytes + (int)sizeof(Shared);
+template <int DP> constexpr int kTilesBytes = 2 * Shape<DP>::kQBytes + Shape<DP>::kSlots * Shape<DP>::kKvBytes;
+template <int DP> constexpr int kSmemBytes = kTilesBytes<DP> + (int)sizeof(Shared);
 static_assert(kSmemBytes<128> <= 227 * 1024 && kSmemBytes<64> <= 227 * 1024, "shared memory of a CTA");
 
 // One CTA's partial sums: slot 0 an item that an earlier CTA began, slot 1 an item that a later CTA goes on with.
 struct SplitDesc {
-    int valid, b, h, qt, tok0, n_tok, c_last, wide;
+    int valid, h, r0, tok0, n_tok, c_last, pad[2];
 };
 
 struct Work {
@@ -89,44 +107,15 @@ __device__ __forceinline__ long long head_units(const Chunk& c, const Geometry& 
     return u;
 }
 
-struct Piece {
-    Chunk c;
-    int b, h, qt;
-    int tok0, n_tok;    // tokens of the item
-    int kv0, kv1, nkv;  // key tiles of this CTA's piece, of the whole item
-    int kv_end;         // tokens that any row of the item may see
-    bool wide;
+// Consecutive shares of `total` units: CTA c begins at unit share_start(c).
+struct Shares {
+    long long total, q;
+    int n, r;
 };
-
-// A CTA's share as a sequence of pieces; every role walks it for itself.
-struct Walk {
-    long long left;  // units still to do
-    int b, h, qt, kv;
-    Chunk c;
-};
-
-__device__ __forceinline__ bool next_piece(const AttnArgs& a, const Geometry& g, Walk& w, Piece& p) {
-    if (w.left <= 0) return false;
-    while (w.qt * g.item_tok >= w.c.n_new) {  // past the head's last item
-        w.qt = 0;
-        if (w.c.n_new == 0 || ++w.h == a.n_kv_heads) {
-            w.h = 0;
-            if (++w.b >= a.c.B) return false;
-            w.c = load_chunk(a.c, w.b);
-        }
-    }
-    p.c = w.c; p.b = w.b; p.h = w.h; p.qt = w.qt;
-    p.tok0 = w.qt * g.item_tok;
-    p.n_tok = min(g.item_tok, w.c.n_new - p.tok0);
-    p.wide = p.n_tok > g.tile_tok;
-    p.nkv = key_tiles(w.c, g, w.qt);
-    p.kv_end = w.c.base + p.tok0 + p.n_tok;
-    p.kv0 = w.kv;
-    p.kv1 = (int)min((long long)p.nkv, p.kv0 + w.left);
-    w.left -= p.kv1 - p.kv0;
-    w.kv = 0;
-    ++w.qt;
-    return true;
+__device__ __forceinline__ long long share_start(const Shares& s, int c) { return c * s.q + min(c, s.r); }
+__device__ __forceinline__ int share_owner(const Shares& s, long long unit) {
+    const long long longer = s.r * (s.q + 1);  // units of the first r shares, which hold one more
+    return unit < longer ? (int)(unit / (s.q + 1)) : s.r + (int)((unit - longer) / s.q);
 }
 
 // a wait of a whole warp: all lanes go on, or none
@@ -134,9 +123,21 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, gave_up));
 }
 
-// position of a step's K and V tile in the order of loads (and of use) of a piece
-__device__ __forceinline__ int k_pos(bool wide, int n) { return wide ? (n & ~1) : (n == 0 ? 0 : 2 * n - 1); }
-__device__ __forceinline__ int v_pos(bool wide, int n, int steps) { return wide ? (n | 1) : (n < steps - 1 ? 2 * n + 2 : 2 * steps - 1); }
+// The pages of a piece's boxes, 32 at a time in the lanes of a loading warp, and the 32 after them on their way.
+struct PageWindow {
+    int page, in, page_next, in_next;
+    __device__ __forceinline__ static void fetch(const ChunkArgs& c, int b, int box, int box_keys, int kv_end, int& page, int& in) {
+        const int64_t key = (int64_t)(box + (int)(threadIdx.x & 31)) * box_keys;
+        page = -1;  // a box outside the tensor: zeros
+        in = 0;
+        if (key < kv_end) {
+            const int j = (int)key / c.page_size;
+            in = (int)key - j * c.page_size;
+            if (HVD_IN_BOUNDS(c.dev_error, j, 0, c.table_stride)) page = c.page_table[(int64_t)b * c.table_stride + j];
+            if (page < 0 || page >= c.n_pages) page = -1;
+        }
+    }
+};
 
 // ---------------------------------------------------------------- the kernel
 
@@ -150,299 +151,362 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// visible columns of a key tile, one bit each
-struct Seen {
-    uint32_t w[4];
-};
-
-__device__ __forceinline__ Seen first_columns(int n) {
-    Seen s;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int k = n - 32 * i;
-        s.w[i] = k >= 32 ? 0xffffffffu : (k <= 0 ? 0u : (1u << k) - 1u);
-    }
+// visible columns of a key tile, one bit each: those below n, and the nodes, node j at column at + j (at may be negative)
+__device__ __forceinline__ unsigned long long seen_columns(int n, unsigned long long nodes, int at) {
+    unsigned long long s = n >= 64 ? ~0ull : (n <= 0 ? 0ull : (1ull << n) - 1ull);
+    if (at >= 0 && at < 64) s |= nodes << at;
+    else if (at < 0 && at > -64) s |= nodes >> -at;
     return s;
-}
-
-// bits of `nodes` shifted so that node j is column at + j (at may be negative)
-__device__ __forceinline__ void add_nodes(Seen& s, unsigned long long nodes, int at) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int sh = 32 * i - at;  // first node of word i
-        unsigned long long v = 0ull;
-        if (sh >= 0 && sh < 64) v = nodes >> sh;
-        else if (sh < 0 && sh > -32) v = nodes << (-sh);
-        s.w[i] |= (uint32_t)v;
-    }
 }
 
 template <typename E, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_tile_kernel(const AttnArgs a, const Work ws, const int box_keys, const int box_tok, const __grid_constant__ CUtensorMap map_q,
+attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int box_keys, const int box_tok, const __grid_constant__ CUtensorMap map_q,
                  const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using S = Shape<DP>;
     extern __shared__ __align__(1024) unsigned char dyn[];
-    Shared& sh = *reinterpret_cast<Shared*>(dyn + (2 + S::kSlots) * S::kTileBytes);
+    Shared& sh = *reinterpret_cast<Shared*>(dyn + kTilesBytes<DP>);
     const uint32_t tiles = smem_addr(dyn);  // 1024-byte aligned: the kernel has no other shared memory
-    const uint32_t ring = tiles + 2 * S::kTileBytes;
+    const uint32_t ring = tiles + 2 * S::kQBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* gave_up = &sh.gave_up;
 
     pdl_trigger();
     if (warp == kMmaWarp) tmem_alloc(smem_addr(&sh.tmem), 512);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kSlots; ++i) { mbar_init(smem_addr(&sh.full[i]), 1); mbar_init(smem_addr(&sh.empty[i]), 1); }
-        mbar_init(smem_addr(&sh.q_full), 1);
-        mbar_init(smem_addr(&sh.q_empty), 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_addr(&sh.s_full[i]), 1);
-            mbar_init(smem_addr(&sh.p_full[i]), 4);
-            mbar_init(smem_addr(&sh.o_full[i]), 1);
+    if (warp == kLoadWarp) {
+        if (lane < 3) tma_prefetch_map(lane == 0 ? &map_q : (lane == 1 ? &map_k : &map_v));
+        if (lane < S::kSlots) { mbar_init(smem_addr(&sh.full[lane]), 1); mbar_init(smem_addr(&sh.empty[lane]), 1); }
+        if (lane < 4) { mbar_init(smem_addr(&sh.s_full[0][lane]), 1); mbar_init(smem_addr(&sh.p_full[0][lane]), 4); mbar_init(smem_addr(&sh.o_full[0][lane]), 1); }
+        if (lane < kPieces) { mbar_init(smem_addr(&sh.piece_full[lane]), 1); mbar_init(smem_addr(&sh.piece_empty[lane]), kSoftmaxWarps + 2); }
+        if (lane == 0) {
+            mbar_init(smem_addr(&sh.q_full), 1);
+            mbar_init(smem_addr(&sh.q_empty), 1);
+            mbar_init(smem_addr(&sh.stats), kSoftmaxWarps);
+            mbar_init(smem_addr(&sh.o_free), kSoftmaxWarps);
+            mbar_init(smem_addr(&sh.drain), 1);
+            sh.gave_up = 0;
         }
-        mbar_init(smem_addr(&sh.stats), kSoftmaxWarps);
-        mbar_init(smem_addr(&sh.o_free), kSoftmaxWarps);
-        mbar_init(smem_addr(&sh.drain), 1);
         mbar_init_fence();
-        sh.gave_up = 0;
     }
-    if (warp == kLoadWarp && lane < 3) tma_prefetch_map(lane == 0 ? &map_q : (lane == 1 ? &map_k : &map_v));
     pdl_wait();
 
     // ---- this CTA's share: units of all requests before each thread's, then the request that holds the share's first unit
-    Geometry g;
-    g.tile_tok = kTileRows / a.group;
-    if (g.tile_tok > box_tok) g.tile_tok -= g.tile_tok % box_tok;
-    g.item_tok = 2 * g.tile_tok;
     const int per = (a.c.B + kThreads - 1) / kThreads;
     const int b0 = min(a.c.B, (int)threadIdx.x * per), b1 = min(a.c.B, b0 + per);
     long long mine = 0;
     for (int b = b0; b < b1; ++b) mine += head_units(load_chunk(a.c, b), g) * a.n_kv_heads;
-    long long upto = mine;
+    long long upto_b = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += t;
+        const long long t = __shfl_up_sync(0xffffffffu, upto_b, d);
+        if (lane >= d) upto_b += t;
     }
-    if (lane == 31) sh.warp_sum[warp] = upto;
+    if (lane == 31) sh.warp_sum[warp] = upto_b;
     __syncthreads();
-    long long total = 0, before = upto - mine;
+    Shares shares;
+    shares.total = 0;
+    long long before = upto_b - mine;
+#pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) {
-        if (i < warp) before += sh.warp_sum[i];
-        total += sh.warp_sum[i];
+        const long long w = sh.warp_sum[i];
+        if (i < warp) before += w;
+        shares.total += w;
     }
-    const int n_cta = (int)min((long long)gridDim.x, total);
+    shares.n = (int)min((long long)gridDim.x, shares.total);
     const int cta = blockIdx.x;
-    const long long first = cta < n_cta ? cta * total / n_cta : 0;
-    const long long last = cta < n_cta ? (cta + 1) * total / n_cta : 0;
-    if (cta < n_cta && first >= before && first < before + mine) {
-        long long off = first - before;
-        int b = b0;
-        for (; b < b1 - 1; ++b) {
-            const long long u = head_units(load_chunk(a.c, b), g) * a.n_kv_heads;
-            if (off < u) break;
-            off -= u;
+    long long first = 0, last = 0;
+    if (cta < shares.n) {
+        shares.q = shares.total / shares.n;
+        shares.r = (int)(shares.total - shares.q * shares.n);
+        first = share_start(shares, cta);
+        last = share_start(shares, cta + 1);
+        if (first >= before && first < before + mine) {
+            long long off = first - before;
+            int b = b0;
+            for (; b < b1 - 1; ++b) {
+                const long long u = head_units(load_chunk(a.c, b), g) * a.n_kv_heads;
+                if (off < u) break;
+                off -= u;
+            }
+            sh.start_b = b;
+            sh.start_off = off;
         }
-        sh.start_b = b;
-        sh.start_off = off;
     }
     if (threadIdx.x == 0) ws.desc[cta].valid = 0;
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = sh.tmem;
-
-    Walk walk = {};
-    walk.left = last - first;
-    if (walk.left > 0) {
-        walk.b = sh.start_b;
-        walk.c = load_chunk(a.c, walk.b);
-        long long off = sh.start_off;
-        const long long hu = head_units(walk.c, g);
-        walk.h = (int)(off / hu);
-        off -= walk.h * hu;
-        for (;; ++walk.qt) {
-            const int u = key_tiles(walk.c, g, walk.qt);
-            if (off < u) break;
-            off -= u;
-        }
-        walk.kv = (int)off;
-    }
     const uint32_t full0 = smem_addr(&sh.full[0]), empty0 = smem_addr(&sh.empty[0]);
-    Piece p;
 
     if (warp >= kSoftmaxWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == kLoadWarp) {
-        // ------------------------------------------------------------ loads
-        int pos = 0, items = 0;  // ring position of the piece's first tile; pieces done
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int n_box = kTileKeys / box_keys;
-        bool ok = true;
-        while (ok && next_piece(a, g, walk, p)) {
-            const int tiles_n = p.kv1 - p.kv0;
-            const int* table = a.c.page_table + (int64_t)p.b * a.c.table_stride;
-            auto load = [&](const CUtensorMap* map, int at, int tile) {  // one K or V tile into ring position `at`
-                const int slot = at % S::kSlots, round = at / S::kSlots;
-                const uint32_t bar = full0 + 8 * slot;
-                const int key = tile * kTileKeys + lane * box_keys;
-                const bool need = lane < n_box && key < p.kv_end;
-                int page = -1, in = 0;
-                if (need) {
-                    const int j = key / a.c.page_size;
-                    in = key - j * a.c.page_size;
-                    if (HVD_IN_BOUNDS(a.c.dev_error, j, 0, a.c.table_stride)) page = table[j];
-                    if (page < 0 || page >= a.c.n_pages) page = -1;  // the box lies outside the tensor: zeros
+        // a piece's K or V tiles into their ring, from ring position `pos` on; after_first() runs behind the first tile
+        auto load_tiles = [&](const Piece& p, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto after_first) {
+            const int kv_end = p.base + p.tok0 + p.n_tok, n = p.kv1 - p.kv0, box0 = p.kv0 * n_box;
+            PageWindow w;
+            PageWindow::fetch(a.c, p.b, box0, box_keys, kv_end, w.page, w.in);
+            PageWindow::fetch(a.c, p.b, box0 + 32, box_keys, kv_end, w.page_next, w.in_next);
+            int slot = pos % slots, round = pos / slots;
+            for (int i = 0; i < n; ++i) {
+                const int at = i * n_box;  // box within the piece
+                if (i > 0 && (at & 31) == 0) {
+                    w.page = w.page_next;
+                    w.in = w.in_next;
+                    PageWindow::fetch(a.c, p.b, box0 + at + 32, box_keys, kv_end, w.page_next, w.in_next);
                 }
-                if (!warp_wait(empty0 + 8 * slot, (round & 1) ^ 1, gave_up)) return false;
-                const int boxes = __popc(__ballot_sync(0xffffffffu, need));
-                if (lane == 0) mbar_expect(bar, (uint32_t)(boxes * box_keys * 128 * S::kHalves));
+                const int page = __shfl_sync(0xffffffffu, w.page, (at + lane) & 31), in = __shfl_sync(0xffffffffu, w.in, (at + lane) & 31);
+                const int keys = kv_end - (p.kv0 + i) * kTileKeys;  // of the item, from this tile on
+                const int boxes = keys >= kTileKeys ? n_box : (keys - 1) / box_keys + 1;
+                if (!warp_wait(empty + 8 * slot, (round & 1) ^ 1, gave_up)) return false;
+                if (lane == 0) mbar_expect(full + 8 * slot, (uint32_t)(boxes * box_keys * 128 * S::kHalves));
                 __syncwarp();
-                if (need) {
+                if (lane < boxes) {
+                    const uint32_t dst = base + slot * S::kKvBytes + lane * box_keys * 128;
 #pragma unroll
-                    for (int hf = 0; hf < S::kHalves; ++hf)
-                        tma_load_4d(ring + slot * S::kTileBytes + hf * S::kHalfBytes + lane * box_keys * 128, map, bar, hf * 64, in, p.h, page);
+                    for (int hf = 0; hf < S::kHalves; ++hf) tma_load_4d(dst + hf * S::kKvHalf, map, full + 8 * slot, hf * 64, in, p.h, page);
                 }
-                return true;
-            };
-            // the first keys do not wait for the previous item's queries to be done with
-            ok = load(&map_k, pos, p.kv0);
-            ok = ok && warp_wait(smem_addr(&sh.q_empty), (items & 1) ^ 1, gave_up);
-            if (!ok) break;
-            const int per_tile = g.tile_tok, n_tiles = p.wide ? 2 : 1;
-            int q_boxes = 0;
-            for (int t = 0; t < n_tiles; ++t) q_boxes += (min(per_tile, p.n_tok - t * per_tile) + box_tok - 1) / box_tok;
-            if (lane == 0) mbar_expect(smem_addr(&sh.q_full), (uint32_t)(q_boxes * box_tok * a.group * 128 * S::kHalves));
-            __syncwarp();
-            for (int t = 0; t < n_tiles; ++t) {
-                const int nb = (min(per_tile, p.n_tok - t * per_tile) + box_tok - 1) / box_tok;
-                for (int i = lane; i < nb * S::kHalves; i += 32) {
-                    const int bx = i / S::kHalves, hf = i % S::kHalves;
-                    tma_load_4d(tiles + t * S::kTileBytes + hf * S::kHalfBytes + bx * box_tok * a.group * 128, &map_q, smem_addr(&sh.q_full), hf * 64,
-                                0, (int)(p.c.r0 + p.tok0 + t * per_tile + bx * box_tok), p.h);
-                }
+                __syncwarp();
+                if (i == 0 && !after_first()) return false;
+                if (++slot == slots) { slot = 0; ++round; }
             }
-            if (p.wide) {
-                ok = load(&map_v, pos + 1, p.kv0);
-                for (int j = 1; ok && j < tiles_n; ++j)
-                    ok = load(&map_k, pos + 2 * j, p.kv0 + j) && load(&map_v, pos + 2 * j + 1, p.kv0 + j);
-            } else {
-                if (tiles_n > 1) ok = load(&map_k, pos + 1, p.kv0 + 1);
-                for (int j = 0; ok && j < tiles_n; ++j) {
-                    ok = load(&map_v, pos + v_pos(false, j, tiles_n), p.kv0 + j);
-                    if (ok && j + 2 < tiles_n) ok = load(&map_k, pos + k_pos(false, j + 2), p.kv0 + j + 2);
-                }
-            }
-            pos += 2 * tiles_n;
-            ++items;
-        }
-        if (!ok) {  // gave up: a bounded wait for every slot's last load before the shared memory is given back
+            return true;
+        };
+        auto drain_loads = [&]() {  // gave up: time for the loads in flight to land before the shared memory is given back
             const unsigned long long t0 = now_ns();
             while (now_ns() - t0 < kWaitLimitNs / 100) {}
-        }
-    } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------ products
-        if (elect_one()) {
-            const bool f16 = sizeof(E) == 2 && std::is_same<E, __half>::value;
-            const int ksteps = (a.head_dim + 15) / 16;
-            const uint32_t qk_desc = instr_desc(f16, 128, kTileKeys, false), pv_desc = instr_desc(f16, 128, ksteps * 16, true);
-            int pos = 0, items = 0, steps_done[2] = {0, 0};
+        };
+        if (warp == kLoadWarp) {
+            // -------------------------------------------------------- work and loads
+            long long left = last - first;
+            int b = 0, h = 0, qt = 0, kv = 0, pos = 0, items = 0;  // pos: position in the K ring
+            Chunk c = {};
+            if (left > 0) {
+                b = sh.start_b;
+                c = load_chunk(a.c, b);
+                long long off = sh.start_off;
+                const long long hu = head_units(c, g);
+                h = (int)(off / hu);
+                off -= h * hu;
+                for (;; ++qt) {
+                    const int u = key_tiles(c, g, qt);
+                    if (off < u) break;
+                    off -= u;
+                }
+                kv = (int)off;
+            }
             bool ok = true;
-            while (ok && next_piece(a, g, walk, p)) {
-                const int tiles_n = p.kv1 - p.kv0, steps = p.wide ? 2 * tiles_n : tiles_n;
-                auto scores = [&](int n) {  // S = Q K^T of step n
-                    const int s = n & 1, at = pos + k_pos(p.wide, n), slot = at % S::kSlots;
-                    if (!mbar_wait(full0 + 8 * slot, (at / S::kSlots) & 1, gave_up)) return false;
-                    fence_after_sync();
-                    const uint32_t qa = tiles + (p.wide ? s : 0) * S::kTileBytes, kb = ring + slot * S::kTileBytes;
-                    for (int k = 0; k < ksteps; ++k) {
-                        const uint32_t off = (k >> 2) * S::kHalfBytes + (k & 3) * 32;
-                        mma_ss(tmem + s * 128, operand_desc(qa + off, 16), operand_desc(kb + off, 16), qk_desc, k > 0);
+            for (;; ++items) {
+                // the next piece
+                Piece p = {};
+                if (left > 0) {
+                    while (qt * g.item_tok >= c.n_new) {  // past the head's last item
+                        qt = 0;
+                        if (c.n_new == 0 || ++h == a.n_kv_heads) {
+                            h = 0;
+                            c = load_chunk(a.c, ++b);
+                        }
                     }
-                    mma_commit(smem_addr(&sh.s_full[s]));
-                    if (!p.wide || s == 1) mma_commit(empty0 + 8 * slot);
-                    if (n == steps - 1) mma_commit(smem_addr(&sh.q_empty));
+                    p.b = b; p.h = h; p.qt = qt; p.r0 = (int)c.r0; p.base = c.base;
+                    p.tok0 = qt * g.item_tok;
+                    p.n_tok = min(g.item_tok, c.n_new - p.tok0);
+                    p.nkv = key_tiles(c, g, qt);
+                    p.kv0 = kv;
+                    p.kv1 = (int)min((long long)p.nkv, kv + left);
+                    left -= p.kv1 - p.kv0;
+                    p.c_last = p.kv1 < p.nkv ? share_owner(shares, last + (p.nkv - p.kv1) - 1) : cta;
+                    kv = 0;
+                    ++qt;
+                }
+                const int ps = items % kPieces;
+                ok = warp_wait(smem_addr(&sh.piece_empty[ps]), ((items / kPieces) & 1) ^ 1, gave_up);
+                if (!ok) break;
+                if (lane == 0) { sh.piece[ps] = p; mbar_arrive(smem_addr(&sh.piece_full[ps])); }
+                if (p.n_tok == 0) break;
+                // the queries go ahead of the second key tile: the first does not wait for the item before to be done with its own
+                auto load_q = [&]() {
+                    if (!warp_wait(smem_addr(&sh.q_empty), (items & 1) ^ 1, gave_up)) return false;
+                    const int n0 = (min(g.tile_tok, p.n_tok) + box_tok - 1) / box_tok;
+                    const int n1 = p.n_tok > g.tile_tok ? (p.n_tok - g.tile_tok + box_tok - 1) / box_tok : 0;
+                    if (lane == 0) mbar_expect(smem_addr(&sh.q_full), (uint32_t)((n0 + n1) * box_tok * a.group * 128 * S::kHalves));
+                    __syncwarp();
+                    for (int x = lane; x < n0 + n1; x += 32) {
+                        const int t = x >= n0, bx = x - (t ? n0 : 0);
+                        const uint32_t dst = tiles + t * S::kQBytes + bx * box_tok * a.group * 128;
+#pragma unroll
+                        for (int hf = 0; hf < S::kHalves; ++hf)
+                            tma_load_4d(dst + hf * S::kQHalf, &map_q, smem_addr(&sh.q_full), hf * 64, 0, p.r0 + p.tok0 + t * g.tile_tok + bx * box_tok, p.h);
+                    }
                     return true;
                 };
-                ok = mbar_wait(smem_addr(&sh.q_full), items & 1, gave_up) && scores(0) && (steps == 1 || scores(1));
-                for (int n = 0; ok && n < steps; ++n) {
-                    const int s = n & 1, at = pos + v_pos(p.wide, n, steps), slot = at % S::kSlots;
-                    ok = mbar_wait(smem_addr(&sh.p_full[s]), steps_done[s] & 1, gave_up) && mbar_wait(full0 + 8 * slot, (at / S::kSlots) & 1, gave_up);
-                    if (ok && n == 0) ok = mbar_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);  // the last item's sums are read
-                    if (!ok) break;
-                    fence_after_sync();
-                    const uint32_t vb = ring + slot * S::kTileBytes;
-#pragma unroll
-                    for (int k = 0; k < kTileKeys / 16; ++k)
-                        mma_ts(tmem + 256 + s * 128, tmem + s * 128 + 8 * k, operand_desc(vb + k * 2048, S::kHalfBytes), pv_desc, n >= 2 || k > 0);
-                    mma_commit(smem_addr(&sh.o_full[s]));
-                    if (!p.wide || s == 1) mma_commit(empty0 + 8 * slot);
-                    ++steps_done[s];
-                    if (n + 2 < steps) ok = scores(n + 2);
-                }
-                pos += 2 * tiles_n;
-                ++items;
+                ok = load_tiles(p, &map_k, ring, full0, empty0, S::kKSlots, pos, load_q);
+                if (!ok) break;
+                pos += p.kv1 - p.kv0;
             }
-            mma_commit(smem_addr(&sh.drain));  // nothing is in flight when tensor memory is freed
-            int never = 0;
-            mbar_wait(smem_addr(&sh.drain), 0, &never);
-            if (never) sh.gave_up = 1;
+            if (!ok) drain_loads();
+        } else if (warp == kLoadVWarp) {
+            int pos = 0;
+            bool ok = true;
+            for (int items = 0;; ++items) {
+                const int ps = items % kPieces;
+                ok = warp_wait(smem_addr(&sh.piece_full[ps]), (items / kPieces) & 1, gave_up);
+                if (!ok) break;
+                const Piece p = sh.piece[ps];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[ps]));
+                if (p.n_tok == 0) break;
+                ok = load_tiles(p, &map_v, ring + S::kKSlots * S::kKvBytes, full0 + 8 * S::kKSlots, empty0 + 8 * S::kKSlots, S::kVSlots, pos,
+                                []() { return true; });
+                if (!ok) break;
+                pos += p.kv1 - p.kv0;
+            }
+            if (!ok) drain_loads();
+        } else if (warp == kMmaWarp) {
+            // -------------------------------------------------------- products
+            if (elect_one()) {
+                const bool f16 = std::is_same<E, __half>::value;
+                const int ksteps = (a.head_dim + 15) / 16;
+                const uint32_t qk_desc = instr_desc(f16, 128, kTileKeys, false), pv_desc = instr_desc(f16, 128, ksteps * 16, true);
+                const uint64_t q_base = operand_desc(tiles, 16), k_base = operand_desc(ring, 16);
+                const uint64_t v_base = operand_desc(ring + S::kKSlots * S::kKvBytes, S::kKvHalf);
+                int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, items = 0;
+                uint32_t qk_done[2] = {0, 0}, pv_done[2] = {0, 0};  // steps of each stream so far
+                bool ok = true;
+                for (;; ++items) {
+                    const int ps = items % kPieces;
+                    ok = mbar_wait(smem_addr(&sh.piece_full[ps]), (items / kPieces) & 1, gave_up);
+                    if (!ok) break;
+                    const Piece& p = sh.piece[ps];
+                    const int n_tok = p.n_tok, n = p.kv1 - p.kv0;
+                    mbar_arrive(smem_addr(&sh.piece_empty[ps]));
+                    if (n_tok == 0) break;
+                    const bool wide = n_tok > g.tile_tok;
+                    const int steps = wide ? 2 * n : n;
+                    ok = mbar_wait(smem_addr(&sh.q_full), items & 1, gave_up);
+                    for (int i = 0; ok && i < steps + 4; ++i) {
+                        if (i >= 4) {  // O += P V of step i - 4
+                            const int st = i - 4, s = st & 1;
+                            const uint32_t buf = pv_done[s] & 1, v_full = full0 + 8 * (S::kKSlots + v_slot);
+                            ok = mbar_wait(smem_addr(&sh.p_full[s][buf]), (pv_done[s] >> 1) & 1, gave_up) &&
+                                 mbar_wait(v_full, v_round & 1, gave_up);
+                            if (ok && st == 0) ok = mbar_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);  // the last item's sums are read
+                            if (!ok) break;
+                            fence_after_sync();
+                            const uint64_t vd = v_base + ((v_slot * S::kKvBytes) >> 4);
+#pragma unroll
+                            for (int k = 0; k < kTileKeys / 16; ++k)
+                                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + buf * 64 + 8 * k, vd + ((k * 2048) >> 4), pv_desc, st >= 2 || k > 0);
+                            mma_commit(smem_addr(&sh.o_full[s][buf]));
+                            if (!wide || s == 1) {
+                                mma_commit(empty0 + 8 * (S::kKSlots + v_slot));
+                                if (++v_slot == S::kVSlots) { v_slot = 0; ++v_round; }
+                            }
+                            ++pv_done[s];
+                        }
+                        if (i < steps) {  // S = Q K^T of step i
+                            const int s = i & 1;
+                            const uint32_t buf = qk_done[s] & 1;
+                            ok = mbar_wait(full0 + 8 * k_slot, k_round & 1, gave_up);
+                            if (!ok) break;
+                            fence_after_sync();
+                            const uint64_t qd = q_base + (((wide ? s : 0) * S::kQBytes) >> 4), kd = k_base + ((k_slot * S::kKvBytes) >> 4);
+#pragma unroll
+                            for (int k = 0; k < DP / 16; ++k)
+                                if (k < ksteps)
+                                    mma_ss(tmem + s * 128 + buf * 64, qd + (((k >> 2) * S::kQHalf + (k & 3) * 32) >> 4),
+                                           kd + (((k >> 2) * S::kKvHalf + (k & 3) * 32) >> 4), qk_desc, k > 0);
+                            mma_commit(smem_addr(&sh.s_full[s][buf]));
+                            if (!wide || s == 1) {
+                                mma_commit(empty0 + 8 * k_slot);
+                                if (++k_slot == S::kKSlots) { k_slot = 0; ++k_round; }
+                            }
+                            if (i == steps - 1) mma_commit(smem_addr(&sh.q_empty));
+                            ++qk_done[s];
+                        }
+                    }
+                    if (!ok) break;
+                }
+                mma_commit(smem_addr(&sh.drain));  // nothing is in flight when tensor memory is freed
+                int never = 0;
+                mbar_wait(smem_addr(&sh.drain), 0, &never);
+                if (never) sh.gave_up = 1;
+            }
+            __syncwarp();
         }
-        __syncwarp();
-    }
     } else {
         // ------------------------------------------------------------ softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int s = warp >> 2, row = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor memory's lanes (bits 16 up)
         const uint32_t s_col = tmem + lanes + s * 128, o_col = tmem + lanes + 256 + s * 128;
-        int pos = 0, items = 0, narrow_items = 0, done[2] = {0, 0};
+        const float2 scale2 = make_float2(a.scale_log2, a.scale_log2);
+        int pos = 0, narrow_items = 0;
+        uint32_t done[2] = {0, 0};  // steps of each stream so far
+        // the last of a stream's steps so far is in its sums.  Up to two products with V are pending, which one barrier's parity
+        // could not tell apart.
+        auto sums_done = [&](int of) {
+            const uint32_t k = done[of] - 1;
+            return warp_wait(smem_addr(&sh.o_full[of][k & 1]), (k >> 1) & 1, gave_up);
+        };
         bool ok = true;
-        while (ok && next_piece(a, g, walk, p)) {
-            const int tiles_n = p.kv1 - p.kv0, steps = p.wide ? 2 * tiles_n : tiles_n;
-            const int tok0 = p.tok0 + (p.wide ? s * g.tile_tok : 0);
+        for (int items = 0;; ++items) {
+            const int ps = items % kPieces;
+            ok = warp_wait(smem_addr(&sh.piece_full[ps]), (items / kPieces) & 1, gave_up);
+            if (!ok) break;
+            const Piece p = sh.piece[ps];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[ps]));
+            if (p.n_tok == 0) break;
+            const bool wide = p.n_tok > g.tile_tok;
+            const int n_tiles = p.kv1 - p.kv0, steps = wide ? 2 * n_tiles : n_tiles;
+            const int tok0 = p.tok0 + (wide ? s * g.tile_tok : 0);
+            const int kv_end = p.base + p.tok0 + p.n_tok;
             const int n_rows = min(g.tile_tok, p.tok0 + p.n_tok - tok0) * a.group;
             const int tok = tok0 + row / a.group, grp = row % a.group;
             const bool valid = row < n_rows, active = (row & ~31) < n_rows;
             // what the row sees: keys below `upto`, in a tree also the nodes on its line
             unsigned long long nodes = 0ull;
-            int upto = p.c.base + tok + 1;
+            int upto = p.base + tok + 1;
             if (a.c.parent) {
                 int depth;
                 const bool reach = !valid || tree_line(a.c, p.b, tok, nodes, depth);
-                upto = reach ? p.c.base + 1 : 0;
+                upto = reach ? p.base + 1 : 0;
             }
             const int all_see = __reduce_min_sync(0xffffffffu, valid ? upto : 0x7fffffff);
             float m = -INFINITY, l = 0.0f;
-            for (int n = s; ok && n < steps; n += 2) {
-                const int tile = p.kv0 + (p.wide ? n >> 1 : n), key0 = tile * kTileKeys;
-                ok = warp_wait(smem_addr(&sh.s_full[s]), done[s] & 1, gave_up);
+            for (int st = s; ok && st < steps; st += 2) {
+                const int j = wide ? st >> 1 : st, key0 = (p.kv0 + j) * kTileKeys;
+                const uint32_t buf = done[s] & 1;
+                ok = warp_wait(smem_addr(&sh.s_full[s][buf]), (done[s] >> 1) & 1, gave_up);
                 if (!ok) break;
                 fence_after_sync();
                 if (active) {
-                    uint32_t x[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32(x[i], s_col + 32 * i);
+                    uint32_t x[2][32];
+                    tmem_ld32(x[0], s_col + buf * 64);
+                    tmem_ld32(x[1], s_col + buf * 64 + 32);
                     tmem_wait_ld(x[0]);
-#pragma unroll
-                    for (int i = 1; i < 4; ++i) tmem_waited(x[i]);
+                    tmem_waited(x[1]);
                     if (key0 + kTileKeys > all_see) {  // some row of the warp does not see the whole tile
-                        Seen seen = first_columns(upto - key0);
-                        if (a.c.parent) add_nodes(seen, nodes, p.c.base + 1 - key0);
+                        const unsigned long long seen = seen_columns(upto - key0, nodes, p.base + 1 - key0);
+                        const uint32_t w[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!((seen.w[i] >> j) & 1u)) x[i][j] = 0xff800000u;
+                            for (int k = 0; k < 32; ++k)
+                                if (!((w[i] >> k) & 1u)) x[i][k] = 0xff800000u;
                     }
                     float top[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        top[i] = __uint_as_float(x[i][0]);
+                        const uint32_t* v = &x[i >> 1][(i & 1) * 16];
+                        top[i] = __uint_as_float(v[0]);
 #pragma unroll
-                        for (int j = 1; j < 32; ++j) top[i] = fmaxf(top[i], __uint_as_float(x[i][j]));
+                        for (int k = 1; k < 15; k += 2) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
+                        top[i] = fmaxf(top[i], __uint_as_float(v[15]));
                     }
                     const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-                    if (n < 2) {
+                    if (st < 2) {
                         m = mt;
                     } else {
                         const bool grown = valid && mt > m + kRescaleAbove;
@@ -451,63 +515,65 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const int box_keys, const int 
                             m = fmaxf(m, mt);
                             const float f = m == -INFINITY ? 1.0f : exp2_approx(old - m);
                             l *= f;
-                            ok = warp_wait(smem_addr(&sh.o_full[s]), (done[s] & 1) ^ 1, gave_up);  // the step before
+                            ok = sums_done(s);
                             fence_after_sync();
                             if (ok) {
-#pragma unroll
+#pragma unroll 1
                                 for (int i = 0; i < DP / 32; ++i) {
                                     uint32_t o[32];
                                     tmem_ld32(o, o_col + 32 * i);
                                     tmem_wait_ld(o);
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
                                     tmem_st32(o_col + 32 * i, o);
                                 }
                             }
                         }
                     }
-                    const float shift = m == -INFINITY ? 0.0f : m;
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const float shift = m == -INFINITY ? 0.0f : -m;
+                    const float2 shift2 = make_float2(shift, shift);
+                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         uint32_t w[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float p0 = exp2_approx(fmaf(__uint_as_float(x[i][2 * j]), a.scale_log2, -shift));
-                            const float p1 = exp2_approx(fmaf(__uint_as_float(x[i][2 * j + 1]), a.scale_log2, -shift));
-                            sum[j & 3] += p0 + p1;
-                            w[j] = pack2<E>(p0, p1);
+                        for (int k = 0; k < 16; ++k) {
+                            float2 e = fma2(make_float2(__uint_as_float(x[i][2 * k]), __uint_as_float(x[i][2 * k + 1])), scale2, shift2);
+                            e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            sum[k & 1] = add2(sum[k & 1], e);
+                            w[k] = pack2<E>(e.x, e.y);
                         }
-                        tmem_st16(s_col + 16 * i, w);
+                        tmem_st16(s_col + buf * 64 + 16 * i, w);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    sum[0] = add2(sum[0], sum[1]);
+                    l += sum[0].x + sum[0].y;
                     tmem_wait_st();
                 }
                 // slots at and behind the item's last key may hold anything: 0 * NaN must not reach the sums
-                if (key0 + kTileKeys > p.kv_end && (!p.wide || s == 0)) {
-                    const int at = pos + v_pos(p.wide, n, steps), slot = at % S::kSlots;
-                    ok = ok && warp_wait(full0 + 8 * slot, (at / S::kSlots) & 1, gave_up);
-                    const int keep = p.kv_end - key0;  // rows that stay
-                    for (int i = row; i < (kTileKeys - keep) * 8 * S::kHalves; i += 128) {
-                        const int hf = i / ((kTileKeys - keep) * 8), r = i - hf * (kTileKeys - keep) * 8;
-                        const uint32_t at_b = ring + slot * S::kTileBytes + hf * S::kHalfBytes + keep * 128 + r * 16;
-                        if (ok) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at_b), "r"(0) : "memory");
-                    }
+                if (key0 + kTileKeys > kv_end && (!wide || s == 0)) {
+                    const int at = pos + j, slot = at % S::kVSlots;
+                    ok = ok && warp_wait(full0 + 8 * (S::kKSlots + slot), (at / S::kVSlots) & 1, gave_up);
+                    const int keep = kv_end - key0, part = (kTileKeys - keep) * 8;  // rows that stay; 16-byte pieces per half to clear
+                    if (ok)
+                        for (int i = row; i < part * S::kHalves; i += 128) {
+                            const int hf = i >= part, r = i - hf * part;
+                            const uint32_t at_b = ring + (S::kKSlots + slot) * S::kKvBytes + hf * S::kKvHalf + keep * 128 + r * 16;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at_b), "r"(0) : "memory");
+                        }
                     fence_async_proxy();
                 }
                 fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[s]));
+                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[s][buf]));
                 ++done[s];
             }
+            if (!ok) break;
             // the other stream's steps, for its barrier's parity
             const int steps_of[2] = {(steps + 1) / 2, steps / 2};
             done[s ^ 1] += steps_of[s ^ 1];
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
-            float* const part_o = ws.o + ((int64_t)(2 * cta + (has_first ? 1 : 0)) * 256) * DP;
-            float2* const part_ml = ws.ml + (int64_t)(2 * cta + (has_first ? 1 : 0)) * 256;
-            if (!p.wide) {  // maxima and sums of both streams, once every warp is through with the item before
-                if (items > 0) ok = ok && warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
+            if (!wide) {  // maxima and sums of both streams, once every warp is through with the item before
+                if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
                 sh.m[s][row] = m;
                 sh.l[s][row] = l;
                 __syncwarp();
@@ -515,73 +581,68 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const int box_keys, const int 
                 ok = ok && warp_wait(smem_addr(&sh.stats), narrow_items & 1, gave_up);
                 ++narrow_items;
             }
-            if (steps_of[0] && (!p.wide || s == 0)) ok = ok && warp_wait(smem_addr(&sh.o_full[0]), (done[0] & 1) ^ 1, gave_up);
-            if (steps_of[1] && (!p.wide || s == 1)) ok = ok && warp_wait(smem_addr(&sh.o_full[1]), (done[1] & 1) ^ 1, gave_up);
+            if (steps_of[0] && (!wide || s == 0)) ok = ok && sums_done(0);
+            if (steps_of[1] && (!wide || s == 1)) ok = ok && sums_done(1);
+            if (!ok) break;
             fence_after_sync();
-            if (ok && active) {
+            if (active) {
                 float f0 = 1.0f, f1 = 0.0f;  // weights of the sums read below
-                if (!p.wide) {
+                if (!wide) {
                     const float m0 = sh.m[0][row], m1 = sh.m[1][row];
                     m = fmaxf(m0, m1);
                     f0 = m0 == -INFINITY ? 0.0f : exp2_approx(m0 - m);
                     f1 = m1 == -INFINITY ? 0.0f : exp2_approx(m1 - m);
                     l = sh.l[0][row] * f0 + (f1 > 0.0f ? sh.l[1][row] * f1 : 0.0f);
                 }
-                const bool two = !p.wide && steps > 1;
-                const int64_t out_row = p.c.r0 + tok;
+                const bool two = !wide && steps > 1;
+                const int64_t out_row = p.r0 + tok;
                 const int head = p.h * a.group + grp;
+                const int64_t part_row = (int64_t)(2 * cta + (has_first ? 1 : 0)) * 256 + (wide ? s * 128 : 0) + row;
                 if (whole) {
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
                     f0 *= inv;
                     f1 *= inv;
-                    if (valid && a.lse && (p.wide || s == 0)) a.lse[out_row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
-                } else if (valid && (p.wide || s == 0)) {
-                    part_ml[(p.wide ? s * 128 : 0) + row] = make_float2(m, l);
+                    if (valid && a.lse && (wide || s == 0)) a.lse[out_row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                } else if (valid && (wide || s == 0)) {
+                    ws.ml[part_row] = make_float2(m, l);
                 }
                 E* const out = reinterpret_cast<E*>(a.out.p) + out_row * a.out.row_stride + (int64_t)head * a.out.head_stride;
-                float* const po = part_o + (int64_t)((p.wide ? s * 128 : 0) + row) * DP;
-                const int c_lo = p.wide ? 0 : s * (DP / 2), c_hi = p.wide ? DP : c_lo + DP / 2;
-                const uint32_t o0 = tmem + lanes + 256 + (p.wide ? s * 128 : 0);
+                float* const po = ws.o + part_row * DP;
+                const int c_lo = wide ? 0 : s * (DP / 2), c_hi = wide ? DP : c_lo + DP / 2;
+                const uint32_t o0 = tmem + lanes + 256 + (wide ? s * 128 : 0);
 #pragma unroll 1
                 for (int c = c_lo; c < c_hi && c < a.head_dim; c += 32) {
-                    uint32_t v[32];
+                    uint32_t v[32], v1[32];
                     tmem_ld32(v, o0 + c);
+                    if (two) tmem_ld32(v1, o0 + 128 + c);
                     tmem_wait_ld(v);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f0);
                     if (two) {
-                        uint32_t v1[32];
-                        tmem_ld32(v1, o0 + 128 + c);
-                        tmem_wait_ld(v1);
+                        tmem_waited(v1);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * f0 + __uint_as_float(v1[j]) * f1);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * f0);
+                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(v1[k]) * f1);
                     }
                     if (!valid) continue;
                     if (whole) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            if (c + j < a.head_dim)
-                                *reinterpret_cast<uint4*>(out + c + j) =
-                                    make_uint4(pack2<E>(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), pack2<E>(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])),
-                                               pack2<E>(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5])), pack2<E>(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
+                        for (int k = 0; k < 32; k += 8)
+                            if (c + k < a.head_dim)
+                                *reinterpret_cast<uint4*>(out + c + k) =
+                                    make_uint4(pack2<E>(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), pack2<E>(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])),
+                                               pack2<E>(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack2<E>(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            if (c + j < a.head_dim) *reinterpret_cast<uint4*>(po + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        for (int k = 0; k < 32; k += 4)
+                            if (c + k < a.head_dim) *reinterpret_cast<uint4*>(po + c + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                     }
                 }
             }
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.o_free));
-            if (threadIdx.x == 0 && has_first && !has_last) {
-                // the CTA that holds the item's last unit; this piece is the share's last
-                const long long last_unit = last + (p.nkv - p.kv1) - 1;
-                ws.desc[cta] = SplitDesc{1, p.b, p.h, p.qt, p.tok0, p.n_tok, (int)(((last_unit + 1) * n_cta - 1) / total), p.wide};
-            }
-            pos += 2 * tiles_n;
-            ++items;
+            if (threadIdx.x == 0 && has_first && !has_last) ws.desc[cta] = SplitDesc{1, p.h, p.r0, p.tok0, p.n_tok, p.c_last, {0, 0}};
+            pos += n_tiles;
         }
     }
     fence_before_sync();
@@ -603,45 +664,61 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
     if (blockIdx.x < (unsigned)n_cta) {
         const SplitDesc d = ws.desc[blockIdx.x];
         if (d.valid) {
-            const Chunk c = load_chunk(a.c, d.b);
             const int rows = d.n_tok * a.group, n = d.c_last - (int)blockIdx.x + 1;
             for (int r = part; r < rows; r += n_part) {
                 // row r of the item: token r / group; its place among the partial sums
                 const int t = r / a.group, grp = r - t * a.group;
                 const int place = t < tile_tok ? r : 128 + r - tile_tok * a.group;
                 auto slot = [&](int i) { return (int64_t)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)) * 256 + place; };
-                float m = -INFINITY;
-                for (int i = lane; i < n; i += 32) m = fmaxf(m, ws.ml[slot(i)].x);
+                const float* const o = ws.o + lane * kPerLane;
+                const bool mine = lane * kPerLane < a.head_dim;
+                float acc[kPerLane] = {}, l = 0.0f, m = -INFINITY;
+                for (int i0 = 0; i0 < n; i0 += 32) {  // 32 pieces at a time, rescaled to the largest maximum so far
+                    const float2 ml = i0 + lane < n ? ws.ml[slot(i0 + lane)] : make_float2(-INFINITY, 0.0f);
+                    float mx = ml.x;
 #pragma unroll
-                for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-                float acc[kPerLane] = {}, l = 0.0f;
-                for (int i0 = 0; i0 < n; i0 += 32) {
-                    float f = 0.0f, li = 0.0f;
-                    if (i0 + lane < n) {
-                        const float2 ml = ws.ml[slot(i0 + lane)];
-                        f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
-                        li = ml.y * f;
-                    }
+                    for (int k = 16; k; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+                    const float old = m;
+                    m = fmaxf(m, mx);
+                    const float keep = old == -INFINITY ? 0.0f : exp2f(old - m), f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
+                    l *= keep;
+#pragma unroll
+                    for (int k = 0; k < kPerLane; ++k) acc[k] *= keep;
+                    float li = ml.y * f;
+#pragma unroll
+                    for (int k = 16; k; k >>= 1) li += __shfl_xor_sync(0xffffffffu, li, k);
+                    l += li;
                     const int e = min(32, n - i0);
-                    for (int i = 0; i < e; ++i) {
-                        const float fi = __shfl_sync(0xffffffffu, f, i);
-                        l += __shfl_sync(0xffffffffu, li, i);
-                        const float* o = ws.o + slot(i0 + i) * DP + lane * kPerLane;
-                        if (lane * kPerLane < a.head_dim) {
-                            if (kPerLane == 4) {
-                                const float4 v = *reinterpret_cast<const float4*>(o);
-                                acc[0] += v.x * fi; acc[1] += v.y * fi; acc[2 % kPerLane] += v.z * fi; acc[3 % kPerLane] += v.w * fi;
+                    for (int i = 0; i < e; i += 8) {  // eight loads in flight
+                        float v[8][kPerLane];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            if (i + u < e && mine) {
+                                const float* q = o + slot(i0 + i + u) * DP;
+                                if constexpr (kPerLane == 4) {
+                                    const float4 w = *reinterpret_cast<const float4*>(q);
+                                    v[u][0] = w.x; v[u][1] = w.y; v[u][2] = w.z; v[u][3] = w.w;
+                                } else {
+                                    const float2 w = *reinterpret_cast<const float2*>(q);
+                                    v[u][0] = w.x; v[u][1] = w.y;
+                                }
                             } else {
-                                const float2 v = *reinterpret_cast<const float2*>(o);
-                                acc[0] += v.x * fi; acc[1] += v.y * fi;
+#pragma unroll
+                                for (int k = 0; k < kPerLane; ++k) v[u][k] = 0.0f;
                             }
+                        }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const float fi = __shfl_sync(0xffffffffu, f, (i + u) & 31);
+#pragma unroll
+                            for (int k = 0; k < kPerLane; ++k) acc[k] += v[u][k] * fi;
                         }
                     }
                 }
-                const int64_t row = c.r0 + d.tok0 + t;
+                const int64_t row = d.r0 + d.tok0 + t;
                 const int head = d.h * a.group + grp;
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                if (lane * kPerLane < a.head_dim) {
+                if (mine) {
                     uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<E*>(a.out.p) + row * a.out.row_stride + (int64_t)head * a.out.head_stride + lane * kPerLane);
 #pragma unroll
                     for (int k = 0; k < kPerLane / 2; ++k) out[k] = pack2<E>(acc[2 * k] * inv, acc[2 * k + 1] * inv);
@@ -721,7 +798,7 @@ hvd_status run(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream) {
                            {(uint64_t)c.n_pages, (uint64_t)c.page_stride, 1}};
         if (!encode(&mq, f16, a.q.p, a.head_dim, dq) || !encode(&mk, f16, c.k, a.head_dim, dk) || !encode(&mv, f16, c.v, a.head_dim, dk))
             return fail(ctx, HVD_ERR_INVALID_ARG, "hvd_attn_paged: q or the cache has strides that TMA does not take");
-        e = launch_kernel(pdl, attn_tile_kernel<E, DP>, dim3(n_cta), dim3(kThreads), kSmemBytes<DP>, stream, a, ws, box_keys, box_tok, mq, mk, mv);
+        e = launch_kernel(pdl, attn_tile_kernel<E, DP>, dim3(n_cta), dim3(kThreads), kSmemBytes<DP>, stream, a, ws, Geometry{tile_tok, 2 * tile_tok}, box_keys, box_tok, mq, mk, mv);
         if (e != cudaSuccess) return cuda_fail(ctx, e, "attn_tile_kernel");
     }
     e = launch_kernel(pdl, attn_finish_kernel<E, DP>, dim3(n_cta, 8), dim3(kFinishThreads), 0, stream, a, ws, c.total_rows > 0 ? n_cta : 0, tile_tok);

@@ -7,7 +7,7 @@
 namespace hvd {
 
 constexpr int kTileRows = 128;   // query rows of one tensor-core tile (a row = one token's query head of a group)
-constexpr int kTileKeys = 128;   // keys of one tile
+constexpr int kTileKeys = 64;    // keys of one tile
 constexpr int kTreeRows = 65;    // rows of the largest token tree (k_cap <= 64 nodes and the root)
 
 // One call's chunks and cache, as checked on the host.
