@@ -10,9 +10,10 @@
 //   wide items (more than 128 rows)   the streams are two row tiles that share every key tile
 //   narrow items                      the streams are the even and the odd key tiles of one row tile, joined at the end
 // Tensor memory, 512 columns: scores [stream][buffer][64] (the weights overwrite the scores they come from), sums [stream][128].
-// Roles of the 12 warps: 0-3 and 4-7 softmax, rescaling and output of stream 0 and 1; 8 issues the products; 9 deals out the
-// work and loads queries and keys, 10 the values, box by box through the page table, by TMA into a ring of slots each;
-// 11 only lends its registers.
+// Roles of the 12 warps: 0-3 and 4-7 softmax, rescaling and output of stream 0 and 1; 8 and 9 issue the products of
+// stream 0 and 1 (one issuing thread for both was measured to be the bound: 2400 cycles a tile pair, where the products take
+// 1285); 10 deals out the work and loads queries and keys, 11 the values, box by box through the page table, by TMA into a
+// ring of slots each.
 //
 // Work is counted in key tiles over all (request, head, group of rows) items and dealt to the SMs in equal
 // consecutive shares, whatever the lengths; every CTA finds its share from the lengths itself.  An item that
@@ -31,7 +32,7 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9, kLoadVWarp = 10;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 10, kLoadVWarp = 11;  // kMmaWarp + 1: stream 1
 constexpr int kThreads = 384;
 // registers: 384 threads start with 168 each; the softmax warpgroups take 208, the third keeps 88 (208 + 208 + 88 = 3 * 168)
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
@@ -44,7 +45,10 @@ template <int DP> struct Shape {
     static constexpr int kHalves = DP / 64;                         // 128-byte columns of a tile row
     static constexpr int kQHalf = kTileRows * 128, kQBytes = kHalves * kQHalf;
     static constexpr int kKvHalf = kTileKeys * 128, kKvBytes = kHalves * kKvHalf;
-    static constexpr int kKSlots = DP == 128 ? 5 : 9, kVSlots = DP == 128 ? 5 : 10;  // the rings: 160 or 152 KB
+    // The rings, 160 or 144 KB.  Even, so that a narrow piece's streams, which take every second tile, never share a slot: a stream
+    // waits for a slot's fill by its parity and must have seen the fill before it.
+    static constexpr int kKSlots = DP == 128 ? 4 : 8, kVSlots = DP == 128 ? 6 : 10;
+    static_assert(kKSlots % 2 == 0 && kVSlots % 2 == 0, "see above");
     static constexpr int kSlots = kKSlots + kVSlots;
 };
 constexpr int kMaxSlots = 20;
@@ -175,15 +179,15 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     if (warp == kMmaWarp) tmem_alloc(smem_addr(&sh.tmem), 512);
     if (warp == kLoadWarp) {
         if (lane < 3) tma_prefetch_map(lane == 0 ? &map_q : (lane == 1 ? &map_k : &map_v));
-        if (lane < S::kSlots) { mbar_init(smem_addr(&sh.full[lane]), 1); mbar_init(smem_addr(&sh.empty[lane]), 1); }
+        if (lane < S::kSlots) { mbar_init(smem_addr(&sh.full[lane]), 1); mbar_init(smem_addr(&sh.empty[lane]), 2); }
         if (lane < 4) { mbar_init(smem_addr(&sh.s_full[0][lane]), 1); mbar_init(smem_addr(&sh.p_full[0][lane]), 4); mbar_init(smem_addr(&sh.o_full[0][lane]), 1); }
-        if (lane < kPieces) { mbar_init(smem_addr(&sh.piece_full[lane]), 1); mbar_init(smem_addr(&sh.piece_empty[lane]), kSoftmaxWarps + 2); }
+        if (lane < kPieces) { mbar_init(smem_addr(&sh.piece_full[lane]), 1); mbar_init(smem_addr(&sh.piece_empty[lane]), kSoftmaxWarps + 3); }
         if (lane == 0) {
             mbar_init(smem_addr(&sh.q_full), 1);
-            mbar_init(smem_addr(&sh.q_empty), 1);
+            mbar_init(smem_addr(&sh.q_empty), 2);
             mbar_init(smem_addr(&sh.stats), kSoftmaxWarps);
             mbar_init(smem_addr(&sh.o_free), kSoftmaxWarps);
-            mbar_init(smem_addr(&sh.drain), 1);
+            mbar_init(smem_addr(&sh.drain), 2);
             sh.gave_up = 0;
         }
         mbar_init_fence();
@@ -362,70 +366,78 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 pos += p.kv1 - p.kv0;
             }
             if (!ok) drain_loads();
-        } else if (warp == kMmaWarp) {
-            // -------------------------------------------------------- products
+        } else {
+            // -------------------------------------------------------- products of one stream
+            const int s = warp - kMmaWarp;
             if (elect_one()) {
                 const bool f16 = std::is_same<E, __half>::value;
                 const int ksteps = (a.head_dim + 15) / 16;
                 const uint32_t qk_desc = instr_desc(f16, 128, kTileKeys, false), pv_desc = instr_desc(f16, 128, ksteps * 16, true);
-                const uint64_t q_base = operand_desc(tiles, 16), k_base = operand_desc(ring, 16);
-                const uint64_t v_base = operand_desc(ring + S::kKSlots * S::kKvBytes, S::kKvHalf);
-                int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, items = 0;
-                uint32_t qk_done[2] = {0, 0}, pv_done[2] = {0, 0};  // steps of each stream so far
+                const uint64_t k_base = operand_desc(ring, 16), v_base = operand_desc(ring + S::kKSlots * S::kKvBytes, S::kKvHalf);
+                const uint32_t s_buf = tmem + s * 128, o_buf = tmem + 256 + s * 128;
+                int pos = 0, items = 0;
+                uint32_t done = 0;  // this stream's steps so far
                 bool ok = true;
                 for (;; ++items) {
                     const int ps = items % kPieces;
                     ok = mbar_wait(smem_addr(&sh.piece_full[ps]), (items / kPieces) & 1, gave_up);
                     if (!ok) break;
-                    const Piece& p = sh.piece[ps];
-                    const int n_tok = p.n_tok, n = p.kv1 - p.kv0;
+                    const int n_tok = sh.piece[ps].n_tok, n = sh.piece[ps].kv1 - sh.piece[ps].kv0;
                     mbar_arrive(smem_addr(&sh.piece_empty[ps]));
                     if (n_tok == 0) break;
                     const bool wide = n_tok > g.tile_tok;
-                    const int steps = wide ? 2 * n : n;
+                    // wide: this row tile with every key tile; narrow: the one row tile with every second key tile
+                    const int steps = wide ? n : (n + 1 - s) / 2, stride = wide ? 1 : 2;
+                    const uint64_t q_base = operand_desc(tiles + (wide ? s : 0) * S::kQBytes, 16);
+                    int k_at = pos + (wide ? 0 : s), v_at = k_at;  // ring positions
+                    // a slot is free when both streams are through with it; in a narrow piece one speaks for both
+                    auto release = [&](int slot) {
+                        mma_commit(empty0 + 8 * slot);
+                        if (!wide) mma_commit(empty0 + 8 * slot);
+                    };
                     ok = mbar_wait(smem_addr(&sh.q_full), items & 1, gave_up);
-                    for (int i = 0; ok && i < steps + 4; ++i) {
-                        if (i >= 4) {  // O += P V of step i - 4
-                            const int st = i - 4, s = st & 1;
-                            const uint32_t buf = pv_done[s] & 1, v_full = full0 + 8 * (S::kKSlots + v_slot);
-                            ok = mbar_wait(smem_addr(&sh.p_full[s][buf]), (pv_done[s] >> 1) & 1, gave_up) &&
-                                 mbar_wait(v_full, v_round & 1, gave_up);
-                            if (ok && st == 0) ok = mbar_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);  // the last item's sums are read
+                    for (int i = 0; ok && i < steps + 2; ++i) {
+                        const int ks = k_at % S::kKSlots, vs = v_at % S::kVSlots;
+                        if (i < steps) ok = mbar_wait(full0 + 8 * ks, (k_at / S::kKSlots) & 1, gave_up);
+                        if (ok && i >= 2) {  // O += P V of step i - 2
+                            const uint32_t k = done + i - 2, buf = k & 1;
+                            // the last item's sums are read, by which also all of its V tiles have been there
+                            if (i == 2) ok = mbar_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
+                            ok = ok && mbar_wait(full0 + 8 * (S::kKSlots + vs), (v_at / S::kVSlots) & 1, gave_up) &&
+                                 mbar_wait(smem_addr(&sh.p_full[s][buf]), (k >> 1) & 1, gave_up);
                             if (!ok) break;
                             fence_after_sync();
-                            const uint64_t vd = v_base + ((v_slot * S::kKvBytes) >> 4);
+                            const uint64_t vd = v_base + ((vs * S::kKvBytes) >> 4);
 #pragma unroll
-                            for (int k = 0; k < kTileKeys / 16; ++k)
-                                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + buf * 64 + 8 * k, vd + ((k * 2048) >> 4), pv_desc, st >= 2 || k > 0);
+                            for (int x = 0; x < kTileKeys / 16; ++x)
+                                mma_ts(o_buf, s_buf + buf * 64 + 8 * x, vd + ((x * 2048) >> 4), pv_desc, i > 2 || x > 0);
                             mma_commit(smem_addr(&sh.o_full[s][buf]));
-                            if (!wide || s == 1) {
-                                mma_commit(empty0 + 8 * (S::kKSlots + v_slot));
-                                if (++v_slot == S::kVSlots) { v_slot = 0; ++v_round; }
-                            }
-                            ++pv_done[s];
+                            release(S::kKSlots + vs);
+                            v_at += stride;
                         }
-                        if (i < steps) {  // S = Q K^T of step i
-                            const int s = i & 1;
-                            const uint32_t buf = qk_done[s] & 1;
-                            ok = mbar_wait(full0 + 8 * k_slot, k_round & 1, gave_up);
-                            if (!ok) break;
+                        if (ok && i < steps) {  // S = Q K^T of step i
+                            const uint32_t buf = (done + i) & 1;
                             fence_after_sync();
-                            const uint64_t qd = q_base + (((wide ? s : 0) * S::kQBytes) >> 4), kd = k_base + ((k_slot * S::kKvBytes) >> 4);
+                            const uint64_t kd = k_base + ((ks * S::kKvBytes) >> 4);
 #pragma unroll
-                            for (int k = 0; k < DP / 16; ++k)
-                                if (k < ksteps)
-                                    mma_ss(tmem + s * 128 + buf * 64, qd + (((k >> 2) * S::kQHalf + (k & 3) * 32) >> 4),
-                                           kd + (((k >> 2) * S::kKvHalf + (k & 3) * 32) >> 4), qk_desc, k > 0);
+                            for (int x = 0; x < DP / 16; ++x)
+                                if (x < ksteps)
+                                    mma_ss(s_buf + buf * 64, q_base + (((x >> 2) * S::kQHalf + (x & 3) * 32) >> 4),
+                                           kd + (((x >> 2) * S::kKvHalf + (x & 3) * 32) >> 4), qk_desc, x > 0);
                             mma_commit(smem_addr(&sh.s_full[s][buf]));
-                            if (!wide || s == 1) {
-                                mma_commit(empty0 + 8 * k_slot);
-                                if (++k_slot == S::kKSlots) { k_slot = 0; ++k_round; }
-                            }
+                            release(ks);
                             if (i == steps - 1) mma_commit(smem_addr(&sh.q_empty));
-                            ++qk_done[s];
+                            k_at += stride;
                         }
                     }
                     if (!ok) break;
+                    if (steps == 0) {  // every phase of o_free is waited for, so that none is mistaken for another
+                        ok = mbar_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
+                        if (!ok) break;
+                        mbar_arrive(smem_addr(&sh.q_empty));
+                    }
+                    done += steps;
+                    pos += n;
                 }
                 mma_commit(smem_addr(&sh.drain));  // nothing is in flight when tensor memory is freed
                 int never = 0;
@@ -549,8 +561,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     l += sum[0].x + sum[0].y;
                     tmem_wait_st();
                 }
-                // slots at and behind the item's last key may hold anything: 0 * NaN must not reach the sums
-                if (key0 + kTileKeys > kv_end && (!wide || s == 0)) {
+                // slots at and behind the item's last key may hold anything: 0 * NaN must not reach the sums.  (Wide: both
+                // streams clear the tile, each ahead of its own product.)
+                if (key0 + kTileKeys > kv_end) {
                     const int at = pos + j, slot = at % S::kVSlots;
                     ok = ok && warp_wait(full0 + 8 * (S::kKSlots + slot), (at / S::kVSlots) & 1, gave_up);
                     const int keep = kv_end - key0, part = (kTileKeys - keep) * 8;  // rows that stay; 16-byte pieces per half to clear
@@ -572,8 +585,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             const int steps_of[2] = {(steps + 1) / 2, steps / 2};
             done[s ^ 1] += steps_of[s ^ 1];
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
-            if (!wide) {  // maxima and sums of both streams, once every warp is through with the item before
-                if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
+            // every warp is through with the item before
+            if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
+            if (!wide) {  // maxima and sums of both streams
                 sh.m[s][row] = m;
                 sh.l[s][row] = l;
                 __syncwarp();
