@@ -15,8 +15,8 @@
 // 1285); 10 deals out the work and loads queries and keys, 11 the values, box by box through the page table, by TMA into a
 // ring of slots each.
 //
-// Work is counted in key tiles over all (request, head, group of rows) items and dealt to the SMs in equal
-// consecutive shares, whatever the lengths; every CTA finds its share from the lengths itself.  An item that
+// Work is counted in steps (a row tile with a key tile) over all (request, head, group of rows) items and dealt to the SMs in
+// equal consecutive shares, whatever the lengths; every CTA finds its share from the lengths itself.  An item that
 // several CTAs share leaves partial sums, which attn_finish_kernel joins in the order of the CTAs: no result depends on
 // timing.
 #include <cudaTypedefs.h>
@@ -104,14 +104,18 @@ __device__ __forceinline__ int key_tiles(const Chunk& c, const Geometry& g, int 
     return (c.base + min(c.n_new, (qt + 1) * g.item_tok) - 1) / kTileKeys + 1;
 }
 
-// key tiles of one head of a request
+// row tiles of an item: 1 (narrow) or 2 (wide)
+__device__ __forceinline__ int row_tiles(const Chunk& c, const Geometry& g, int qt) { return c.n_new - qt * g.item_tok > g.tile_tok ? 2 : 1; }
+
+// steps of one head of a request
 __device__ __forceinline__ long long head_units(const Chunk& c, const Geometry& g) {
     long long u = 0;
-    for (int qt = 0; qt * g.item_tok < c.n_new; ++qt) u += key_tiles(c, g, qt);
+    for (int qt = 0; qt * g.item_tok < c.n_new; ++qt) u += (long long)key_tiles(c, g, qt) * row_tiles(c, g, qt);
     return u;
 }
 
-// Consecutive shares of `total` units: CTA c begins at unit share_start(c).
+// Consecutive shares of `total` units: CTA c begins at unit share_start(c).  A wide item is cut between key tiles, so where there are
+// wide items a share has two units at least.
 struct Shares {
     long long total, q;
     int n, r;
@@ -163,6 +167,45 @@ __device__ __forceinline__ unsigned long long seen_columns(int n, unsigned long 
     return s;
 }
 
+// 2^x of two finite numbers on the multiply-add pipe: x = n + f with n the nearest whole number, 2^f as the minimax polynomial of
+// degree 4 on [-1/2, 1/2] (Remez exchange; relative error 2.6e-6), n added to the exponent.  x is held above -126.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    const float2 magic = make_float2(12582912.0f, 12582912.0f), unmagic = make_float2(-12582912.0f, -12582912.0f);  // 1.5 * 2^23
+    x = make_float2(fmaxf(x.x, -126.0f), fmaxf(x.y, -126.0f));
+    const float2 t = add2(x, magic);
+    const float2 f = fma2(add2(t, unmagic), make_float2(-1.0f, -1.0f), x);
+    float2 p = make_float2(0.009570102014629326f, 0.009570102014629326f);
+    p = fma2(p, f, make_float2(0.05591786030632565f, 0.05591786030632565f));
+    p = fma2(p, f, make_float2(0.24024744824991692f, 0.24024744824991692f));
+    p = fma2(p, f, make_float2(0.6931218147429867f, 0.6931218147429867f));
+    p = fma2(p, f, make_float2(0.9999992614469312f, 0.9999992614469312f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// w = exp2(x * scale - m) of a row's 64 scores, rounded to the cache's type and packed, into tensor memory over the scores; returns
+// their sums before rounding.  SHARE: every third pair goes through exp2_poly, which relieves the special function unit (two
+// row tiles of 32 K keys, us: none 96.5, every 8th 93.6, 4th 92.7, 3rd 91.6, 2nd 94.4); no score may be infinite then.
+template <typename E, bool SHARE>
+__device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t dst, float2 scale2, float m) {
+    const float shift = m == -INFINITY ? 0.0f : -m;
+    const float2 shift2 = make_float2(shift, shift);
+    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            float2 e = fma2(make_float2(__uint_as_float(x[i][2 * k]), __uint_as_float(x[i][2 * k + 1])), scale2, shift2);
+            if (SHARE && k % 3 == 2) e = exp2_poly(e);
+            else e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+            sum[k & 1] = add2(sum[k & 1], e);
+            w[k] = pack2<E>(e.x, e.y);
+        }
+        tmem_st16(dst + 16 * i, w);
+    }
+    return add2(sum[0], sum[1]);
+}
+
 template <typename E, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int box_keys, const int box_tok, const __grid_constant__ CUtensorMap map_q,
@@ -198,7 +241,12 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     const int per = (a.c.B + kThreads - 1) / kThreads;
     const int b0 = min(a.c.B, (int)threadIdx.x * per), b1 = min(a.c.B, b0 + per);
     long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += head_units(load_chunk(a.c, b), g) * a.n_kv_heads;
+    bool any_wide = false;
+    for (int b = b0; b < b1; ++b) {
+        const Chunk c = load_chunk(a.c, b);
+        mine += head_units(c, g) * a.n_kv_heads;
+        any_wide = any_wide || c.n_new > g.tile_tok;
+    }
     long long upto_b = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -206,7 +254,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (lane >= d) upto_b += t;
     }
     if (lane == 31) sh.warp_sum[warp] = upto_b;
-    __syncthreads();
+    any_wide = __syncthreads_or(any_wide);
     Shares shares;
     shares.total = 0;
     long long before = upto_b - mine;
@@ -216,7 +264,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (i < warp) before += w;
         shares.total += w;
     }
-    shares.n = (int)min((long long)gridDim.x, shares.total);
+    shares.n = (int)min((long long)gridDim.x, any_wide ? shares.total / 2 : shares.total);
     const int cta = blockIdx.x;
     long long first = 0, last = 0;
     if (cta < shares.n) {
@@ -294,11 +342,15 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 h = (int)(off / hu);
                 off -= h * hu;
                 for (;; ++qt) {
-                    const int u = key_tiles(c, g, qt);
+                    const long long u = (long long)key_tiles(c, g, qt) * row_tiles(c, g, qt);
                     if (off < u) break;
                     off -= u;
                 }
-                kv = (int)off;
+                // a share that begins inside a wide item's step pair begins behind it
+                const int w = row_tiles(c, g, qt);
+                kv = (int)((off + w - 1) / w);
+                left -= kv * w - off;
+                if (kv == key_tiles(c, g, qt)) { kv = 0; ++qt; }
             }
             bool ok = true;
             for (;; ++items) {
@@ -317,9 +369,11 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     p.n_tok = min(g.item_tok, c.n_new - p.tok0);
                     p.nkv = key_tiles(c, g, qt);
                     p.kv0 = kv;
-                    p.kv1 = (int)min((long long)p.nkv, kv + left);
-                    left -= p.kv1 - p.kv0;
-                    p.c_last = p.kv1 < p.nkv ? share_owner(shares, last + (p.nkv - p.kv1) - 1) : cta;
+                    const int w = row_tiles(c, g, qt);
+                    p.kv1 = (int)min((long long)p.nkv, kv + (left + w - 1) / w);
+                    left -= (long long)(p.kv1 - p.kv0) * w;
+                    // the last step pair of the item may begin a share that begins behind it: its first unit has the owner
+                    p.c_last = p.kv1 < p.nkv ? share_owner(shares, last - left + (long long)(p.nkv - p.kv1) * w - w) : cta;
                     kv = 0;
                     ++qt;
                 }
@@ -454,11 +508,11 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         const uint32_t s_col = tmem + lanes + s * 128, o_col = tmem + lanes + 256 + s * 128;
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2);
         int pos = 0, narrow_items = 0;
-        uint32_t done[2] = {0, 0};  // steps of each stream so far
+        uint32_t done = 0, done_other = 0;  // steps of this stream and of the other one so far
         // the last of a stream's steps so far is in its sums.  Up to two products with V are pending, which one barrier's parity
         // could not tell apart.
-        auto sums_done = [&](int of) {
-            const uint32_t k = done[of] - 1;
+        auto sums_done = [&](int of, uint32_t steps_so_far) {
+            const uint32_t k = steps_so_far - 1;
             return warp_wait(smem_addr(&sh.o_full[of][k & 1]), (k >> 1) & 1, gave_up);
         };
         bool ok = true;
@@ -489,8 +543,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             float m = -INFINITY, l = 0.0f;
             for (int st = s; ok && st < steps; st += 2) {
                 const int j = wide ? st >> 1 : st, key0 = (p.kv0 + j) * kTileKeys;
-                const uint32_t buf = done[s] & 1;
-                ok = warp_wait(smem_addr(&sh.s_full[s][buf]), (done[s] >> 1) & 1, gave_up);
+                const uint32_t buf = done & 1;
+                ok = warp_wait(smem_addr(&sh.s_full[s][buf]), (done >> 1) & 1, gave_up);
                 if (!ok) break;
                 fence_after_sync();
                 if (active) {
@@ -499,7 +553,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     tmem_ld32(x[1], s_col + buf * 64 + 32);
                     tmem_wait_ld(x[0]);
                     tmem_waited(x[1]);
-                    if (key0 + kTileKeys > all_see) {  // some row of the warp does not see the whole tile
+                    const bool edge = key0 + kTileKeys > all_see;  // some row of the warp does not see the whole tile
+                    if (edge) {
                         const unsigned long long seen = seen_columns(upto - key0, nodes, p.base + 1 - key0);
                         const uint32_t w[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
@@ -527,7 +582,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                             m = fmaxf(m, mt);
                             const float f = m == -INFINITY ? 1.0f : exp2_approx(old - m);
                             l *= f;
-                            ok = sums_done(s);
+                            ok = sums_done(s, done);  // the step before
                             fence_after_sync();
                             if (ok) {
 #pragma unroll 1
@@ -542,23 +597,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                             }
                         }
                     }
-                    const float shift = m == -INFINITY ? 0.0f : -m;
-                    const float2 shift2 = make_float2(shift, shift);
-                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            float2 e = fma2(make_float2(__uint_as_float(x[i][2 * k]), __uint_as_float(x[i][2 * k + 1])), scale2, shift2);
-                            e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                            sum[k & 1] = add2(sum[k & 1], e);
-                            w[k] = pack2<E>(e.x, e.y);
-                        }
-                        tmem_st16(s_col + buf * 64 + 16 * i, w);
-                    }
-                    sum[0] = add2(sum[0], sum[1]);
-                    l += sum[0].x + sum[0].y;
+                    const float2 sum = edge ? weights<E, false>(x, s_col + buf * 64, scale2, m) : weights<E, true>(x, s_col + buf * 64, scale2, m);
+                    l += sum.x + sum.y;
                     tmem_wait_st();
                 }
                 // slots at and behind the item's last key may hold anything: 0 * NaN must not reach the sums.  (Wide: both
@@ -578,12 +618,10 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[s][buf]));
-                ++done[s];
+                ++done;
             }
             if (!ok) break;
-            // the other stream's steps, for its barrier's parity
-            const int steps_of[2] = {(steps + 1) / 2, steps / 2};
-            done[s ^ 1] += steps_of[s ^ 1];
+            done_other += s ? (steps + 1) / 2 : steps / 2;
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
             // every warp is through with the item before
             if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
@@ -595,8 +633,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 ok = ok && warp_wait(smem_addr(&sh.stats), narrow_items & 1, gave_up);
                 ++narrow_items;
             }
-            if (steps_of[0] && (!wide || s == 0)) ok = ok && sums_done(0);
-            if (steps_of[1] && (!wide || s == 1)) ok = ok && sums_done(1);
+            if (wide || s == 0 || steps > 1) ok = ok && sums_done(s, done);
+            if (!wide && (s == 1 || steps > 1)) ok = ok && sums_done(s ^ 1, done_other);
             if (!ok) break;
             fence_after_sync();
             if (active) {
