@@ -73,8 +73,8 @@ struct Shared {  // behind the tiles
     Piece piece[kPieces];
     uint32_t tmem;
     int gave_up;
-    int start_b;
-    long long start_off;
+    struct { int b, h, qt, kv, r0, n_new, base; } start;  // where the CTA's share begins
+    long long start_left;
     long long warp_sum[kThreads / 32];
     float m[2][128], l[2][128];  // [stream][row]
 };
@@ -114,8 +114,13 @@ __device__ __forceinline__ long long head_units(const Chunk& c, const Geometry& 
     return u;
 }
 
-// Consecutive shares of `total` units: CTA c begins at unit share_start(c).  A wide item is cut between key tiles, so where there are
-// wide items a share has two units at least.
+// 32 bits nearly always do; the 64-bit division is a long way round at the start of a short kernel
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Consecutive shares of `total` units: CTA c begins at unit share_start(c).  A share has two units at least: a wide item is cut
+// between key tiles (two units each), and a narrow one keeps both streams busy.
 struct Shares {
     long long total, q;
     int n, r;
@@ -123,7 +128,7 @@ struct Shares {
 __device__ __forceinline__ long long share_start(const Shares& s, int c) { return c * s.q + min(c, s.r); }
 __device__ __forceinline__ int share_owner(const Shares& s, long long unit) {
     const long long longer = s.r * (s.q + 1);  // units of the first r shares, which hold one more
-    return unit < longer ? (int)(unit / (s.q + 1)) : s.r + (int)((unit - longer) / s.q);
+    return unit < longer ? (int)quotient(unit, s.q + 1) : s.r + (int)quotient(unit - longer, s.q);
 }
 
 // a wait of a whole warp: all lanes go on, or none
@@ -241,11 +246,11 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     const int per = (a.c.B + kThreads - 1) / kThreads;
     const int b0 = min(a.c.B, (int)threadIdx.x * per), b1 = min(a.c.B, b0 + per);
     long long mine = 0;
-    bool any_wide = false;
+    Chunk c0 = {};
     for (int b = b0; b < b1; ++b) {
         const Chunk c = load_chunk(a.c, b);
+        if (b == b0) c0 = c;
         mine += head_units(c, g) * a.n_kv_heads;
-        any_wide = any_wide || c.n_new > g.tile_tok;
     }
     long long upto_b = mine;
 #pragma unroll
@@ -254,7 +259,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (lane >= d) upto_b += t;
     }
     if (lane == 31) sh.warp_sum[warp] = upto_b;
-    any_wide = __syncthreads_or(any_wide);
+    __syncthreads();
     Shares shares;
     shares.total = 0;
     long long before = upto_b - mine;
@@ -264,24 +269,39 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (i < warp) before += w;
         shares.total += w;
     }
-    shares.n = (int)min((long long)gridDim.x, any_wide ? shares.total / 2 : shares.total);
+    shares.n = (int)min((long long)gridDim.x, (shares.total + 1) / 2);
     const int cta = blockIdx.x;
     long long first = 0, last = 0;
     if (cta < shares.n) {
-        shares.q = shares.total / shares.n;
+        shares.q = quotient(shares.total, shares.n);
         shares.r = (int)(shares.total - shares.q * shares.n);
         first = share_start(shares, cta);
         last = share_start(shares, cta + 1);
         if (first >= before && first < before + mine) {
-            long long off = first - before;
+            long long off = first - before, left = last - first, hu = head_units(c0, g);
+            Chunk c = c0;
             int b = b0;
-            for (; b < b1 - 1; ++b) {
-                const long long u = head_units(load_chunk(a.c, b), g) * a.n_kv_heads;
-                if (off < u) break;
-                off -= u;
+            while (off >= hu * a.n_kv_heads) {
+                off -= hu * a.n_kv_heads;
+                c = load_chunk(a.c, ++b);
+                hu = head_units(c, g);
             }
-            sh.start_b = b;
-            sh.start_off = off;
+            const int h = (int)quotient(off, hu);
+            off -= h * hu;
+            int qt = 0, w = row_tiles(c, g, 0);
+            for (long long u; off >= (u = (long long)key_tiles(c, g, qt) * w);) {
+                off -= u;
+                w = row_tiles(c, g, ++qt);
+            }
+            // a share that begins inside a wide item's step pair begins behind it
+            int kv = (int)off;
+            if (w == 2) {
+                kv = (int)((off + 1) >> 1);
+                left -= kv * 2 - off;
+                if (kv == key_tiles(c, g, qt)) { kv = 0; ++qt; }
+            }
+            sh.start = {b, h, qt, kv, (int)c.r0, c.n_new, c.base};
+            sh.start_left = left;
         }
     }
     if (threadIdx.x == 0) ws.desc[cta].valid = 0;
@@ -294,13 +314,14 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     if (warp >= kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int n_box = kTileKeys / box_keys;
-        // a piece's K or V tiles into their ring, from ring position `pos` on; after_first() runs behind the first tile
-        auto load_tiles = [&](const Piece& p, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto after_first) {
+        // a piece's K or V tiles into their ring, from ring position `pos` on; around_first() runs ahead of and behind the first tile
+        auto load_tiles = [&](const Piece& p, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto around_first) {
             const int kv_end = p.base + p.tok0 + p.n_tok, n = p.kv1 - p.kv0, box0 = p.kv0 * n_box;
             PageWindow w;
             PageWindow::fetch(a.c, p.b, box0, box_keys, kv_end, w.page, w.in);
             PageWindow::fetch(a.c, p.b, box0 + 32, box_keys, kv_end, w.page_next, w.in_next);
             int slot = pos % slots, round = pos / slots;
+            if (!around_first(true)) return false;
             for (int i = 0; i < n; ++i) {
                 const int at = i * n_box;  // box within the piece
                 if (i > 0 && (at & 31) == 0) {
@@ -320,7 +341,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     for (int hf = 0; hf < S::kHalves; ++hf) tma_load_4d(dst + hf * S::kKvHalf, map, full + 8 * slot, hf * 64, in, p.h, page);
                 }
                 __syncwarp();
-                if (i == 0 && !after_first()) return false;
+                if (i == 0 && !around_first(false)) return false;
                 if (++slot == slots) { slot = 0; ++round; }
             }
             return true;
@@ -331,26 +352,13 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         };
         if (warp == kLoadWarp) {
             // -------------------------------------------------------- work and loads
-            long long left = last - first;
+            long long left = 0;
             int b = 0, h = 0, qt = 0, kv = 0, pos = 0, items = 0;  // pos: position in the K ring
             Chunk c = {};
-            if (left > 0) {
-                b = sh.start_b;
-                c = load_chunk(a.c, b);
-                long long off = sh.start_off;
-                const long long hu = head_units(c, g);
-                h = (int)(off / hu);
-                off -= h * hu;
-                for (;; ++qt) {
-                    const long long u = (long long)key_tiles(c, g, qt) * row_tiles(c, g, qt);
-                    if (off < u) break;
-                    off -= u;
-                }
-                // a share that begins inside a wide item's step pair begins behind it
-                const int w = row_tiles(c, g, qt);
-                kv = (int)((off + w - 1) / w);
-                left -= kv * w - off;
-                if (kv == key_tiles(c, g, qt)) { kv = 0; ++qt; }
+            if (last > first) {
+                left = sh.start_left;
+                b = sh.start.b; h = sh.start.h; qt = sh.start.qt; kv = sh.start.kv;
+                c.r0 = sh.start.r0; c.n_new = sh.start.n_new; c.base = sh.start.base;
             }
             bool ok = true;
             for (;; ++items) {
@@ -382,8 +390,10 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 if (!ok) break;
                 if (lane == 0) { sh.piece[ps] = p; mbar_arrive(smem_addr(&sh.piece_full[ps])); }
                 if (p.n_tok == 0) break;
-                // the queries go ahead of the second key tile: the first does not wait for the item before to be done with its own
-                auto load_q = [&]() {
+                // a first piece's queries go while its page entries are on their way; later ones go behind the first key tile, which
+                // does not wait for the item before to be done with its own
+                auto load_q = [&](bool ahead) {
+                    if (ahead != (items == 0)) return true;
                     if (!warp_wait(smem_addr(&sh.q_empty), (items & 1) ^ 1, gave_up)) return false;
                     const int n0 = (min(g.tile_tok, p.n_tok) + box_tok - 1) / box_tok;
                     const int n1 = p.n_tok > g.tile_tok ? (p.n_tok - g.tile_tok + box_tok - 1) / box_tok : 0;
@@ -415,7 +425,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[ps]));
                 if (p.n_tok == 0) break;
                 ok = load_tiles(p, &map_v, ring + S::kKSlots * S::kKvBytes, full0 + 8 * S::kKSlots, empty0 + 8 * S::kKSlots, S::kVSlots, pos,
-                                []() { return true; });
+                                [](bool) { return true; });
                 if (!ok) break;
                 pos += p.kv1 - p.kv0;
             }
@@ -853,7 +863,10 @@ hvd_status run(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream) {
         e = launch_kernel(pdl, attn_tile_kernel<E, DP>, dim3(n_cta), dim3(kThreads), kSmemBytes<DP>, stream, a, ws, Geometry{tile_tok, 2 * tile_tok}, box_keys, box_tok, mq, mk, mv);
         if (e != cudaSuccess) return cuda_fail(ctx, e, "attn_tile_kernel");
     }
-    e = launch_kernel(pdl, attn_finish_kernel<E, DP>, dim3(n_cta, 8), dim3(kFinishThreads), 0, stream, a, ws, c.total_rows > 0 ? n_cta : 0, tile_tok);
+    // a warp joins a row at a time: blocks for as many rows as an item can have here, four a warp
+    const int64_t most_rows = c.total_rows * a.group < 256 ? c.total_rows * a.group : 256;
+    const int by = (int)((most_rows + 31) / 32 > 1 ? (most_rows + 31) / 32 : 1);
+    e = launch_kernel(pdl, attn_finish_kernel<E, DP>, dim3(n_cta, by), dim3(kFinishThreads), 0, stream, a, ws, c.total_rows > 0 ? n_cta : 0, tile_tok);
     return e == cudaSuccess ? HVD_OK : cuda_fail(ctx, e, "attn_finish_kernel");
 }
 
