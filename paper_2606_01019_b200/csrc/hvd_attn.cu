@@ -58,8 +58,7 @@ struct Piece {  // what a CTA does of one item
     int r0, base;       // the request's first row, tokens cached before the chunk
     int tok0, n_tok;    // tokens of the item; n_tok = 0: no more work
     int kv0, kv1, nkv;  // key tiles of the piece, of the item
-    int c_last;         // the CTA that holds the item's last tile
-    int pad;
+    int pad[2];
 };
 
 struct Shared {  // behind the tiles
@@ -75,6 +74,7 @@ struct Shared {  // behind the tiles
     int gave_up;
     struct { int b, h, qt, kv, r0, n_new, base; } start;  // where the CTA's share begins
     long long start_left;
+    long long open_unit;  // of the item that the share leaves unfinished: its last tile's first unit
     long long warp_sum[kThreads / 32];
     float m[2][128], l[2][128];  // [stream][row]
 };
@@ -119,8 +119,8 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// Consecutive shares of `total` units: CTA c begins at unit share_start(c).  A share has two units at least: a wide item is cut
-// between key tiles (two units each), and a narrow one keeps both streams busy.
+// Consecutive shares of `total` units: CTA c begins at unit share_start(c).  A wide item is cut between key tiles
+// (two units each), so that where there are wide items a share has two units at least.
 struct Shares {
     long long total, q;
     int n, r;
@@ -141,13 +141,12 @@ struct PageWindow {
     int page, in, page_next, in_next;
     __device__ __forceinline__ static void fetch(const ChunkArgs& c, int b, int box, int box_keys, int kv_end, int& page, int& in) {
         const int64_t key = (int64_t)(box + (int)(threadIdx.x & 31)) * box_keys;
-        page = -1;  // a box outside the tensor: zeros
+        page = -1;
         in = 0;
         if (key < kv_end) {
             const int j = (int)key / c.page_size;
             in = (int)key - j * c.page_size;
             if (HVD_IN_BOUNDS(c.dev_error, j, 0, c.table_stride)) page = c.page_table[(int64_t)b * c.table_stride + j];
-            if (page < 0 || page >= c.n_pages) page = -1;
         }
     }
 };
@@ -188,10 +187,11 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
 }
 
 // w = exp2(x * scale - m) of a row's 64 scores, rounded to the cache's type and packed, into tensor memory over the scores; returns
-// their sums before rounding.  SHARE: every third pair goes through exp2_poly, which relieves the special function unit (two
-// row tiles of 32 K keys, us: none 96.5, every 8th 93.6, 4th 92.7, 3rd 91.6, 2nd 94.4); no score may be infinite then.
-template <typename E, bool SHARE>
-__device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t dst, float2 scale2, float m) {
+// their sums before rounding.  Every third pair goes through exp2_poly, which relieves the special function unit (two
+// row tiles of 32 K keys, us: none 96.5, every 8th 93.6, 4th 92.7, 3rd 91.6, 2nd 94.4).  That makes 2^-126 of a score of -infinity:
+// where there are some (`edge`) those weights are cleared by `seen`.
+template <typename E>
+__device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t dst, float2 scale2, float m, bool edge, unsigned long long seen) {
     const float shift = m == -INFINITY ? 0.0f : -m;
     const float2 shift2 = make_float2(shift, shift);
     float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
@@ -201,10 +201,15 @@ __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t d
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             float2 e = fma2(make_float2(__uint_as_float(x[i][2 * k]), __uint_as_float(x[i][2 * k + 1])), scale2, shift2);
-            if (SHARE && k % 3 == 2) e = exp2_poly(e);
+            if (k % 3 == 2) e = exp2_poly(e);
             else e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
             sum[k & 1] = add2(sum[k & 1], e);
             w[k] = pack2<E>(e.x, e.y);
+        }
+        if (edge) {
+            const uint32_t bits = (uint32_t)(seen >> (32 * i));
+#pragma unroll
+            for (int k = 2; k < 16; k += 3) w[k] &= (((bits >> (2 * k)) & 1u) ? 0xffffu : 0u) | (((bits >> (2 * k + 1)) & 1u) ? 0xffff0000u : 0u);
         }
         tmem_st16(dst + 16 * i, w);
     }
@@ -247,9 +252,11 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     const int b0 = min(a.c.B, (int)threadIdx.x * per), b1 = min(a.c.B, b0 + per);
     long long mine = 0;
     Chunk c0 = {};
+    bool any_wide = false;
     for (int b = b0; b < b1; ++b) {
         const Chunk c = load_chunk(a.c, b);
         if (b == b0) c0 = c;
+        any_wide = any_wide || c.n_new > g.tile_tok;
         mine += head_units(c, g) * a.n_kv_heads;
     }
     long long upto_b = mine;
@@ -259,7 +266,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (lane >= d) upto_b += t;
     }
     if (lane == 31) sh.warp_sum[warp] = upto_b;
-    __syncthreads();
+    any_wide = __syncthreads_or(any_wide);
     Shares shares;
     shares.total = 0;
     long long before = upto_b - mine;
@@ -269,7 +276,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         if (i < warp) before += w;
         shares.total += w;
     }
-    shares.n = (int)min((long long)gridDim.x, (shares.total + 1) / 2);
+    shares.n = (int)min((long long)gridDim.x, any_wide ? (shares.total + 1) / 2 : shares.total);
     const int cta = blockIdx.x;
     long long first = 0, last = 0;
     if (cta < shares.n) {
@@ -329,7 +336,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     w.in = w.in_next;
                     PageWindow::fetch(a.c, p.b, box0 + at + 32, box_keys, kv_end, w.page_next, w.in_next);
                 }
-                const int page = __shfl_sync(0xffffffffu, w.page, (at + lane) & 31), in = __shfl_sync(0xffffffffu, w.in, (at + lane) & 31);
+                int page = __shfl_sync(0xffffffffu, w.page, (at + lane) & 31);
+                const int in = __shfl_sync(0xffffffffu, w.in, (at + lane) & 31);
+                if (page < 0 || page >= a.c.n_pages) page = -1;  // the box lies outside the tensor: zeros
                 const int keys = kv_end - (p.kv0 + i) * kTileKeys;  // of the item, from this tile on
                 const int boxes = keys >= kTileKeys ? n_box : (keys - 1) / box_keys + 1;
                 if (!warp_wait(empty + 8 * slot, (round & 1) ^ 1, gave_up)) return false;
@@ -378,10 +387,13 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     p.nkv = key_tiles(c, g, qt);
                     p.kv0 = kv;
                     const int w = row_tiles(c, g, qt);
-                    p.kv1 = (int)min((long long)p.nkv, kv + (left + w - 1) / w);
+                    p.kv1 = (int)min((long long)p.nkv, kv + ((left + w - 1) >> (w - 1)));
                     left -= (long long)(p.kv1 - p.kv0) * w;
-                    // the last step pair of the item may begin a share that begins behind it: its first unit has the owner
-                    p.c_last = p.kv1 < p.nkv ? share_owner(shares, last - left + (long long)(p.nkv - p.kv1) * w - w) : cta;
+                    if (p.kv0 == 0 && p.kv1 < p.nkv && lane == 0) {
+                        // What joins the pieces has to know the CTA with the item's last tile, by the tile's first unit.  (A share that
+                        // begins with a tile's second unit begins behind it.)
+                        sh.open_unit = last - left + (long long)(p.nkv - p.kv1 - 1) * w;
+                    }
                     kv = 0;
                     ++qt;
                 }
@@ -564,8 +576,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     tmem_wait_ld(x[0]);
                     tmem_waited(x[1]);
                     const bool edge = key0 + kTileKeys > all_see;  // some row of the warp does not see the whole tile
+                    unsigned long long seen = ~0ull;
                     if (edge) {
-                        const unsigned long long seen = seen_columns(upto - key0, nodes, p.base + 1 - key0);
+                        seen = seen_columns(upto - key0, nodes, p.base + 1 - key0);
                         const uint32_t w[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
@@ -607,7 +620,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                             }
                         }
                     }
-                    const float2 sum = edge ? weights<E, false>(x, s_col + buf * 64, scale2, m) : weights<E, true>(x, s_col + buf * 64, scale2, m);
+                    const float2 sum = weights<E>(x, s_col + buf * 64, scale2, m, edge, seen);
                     l += sum.x + sum.y;
                     tmem_wait_st();
                 }
@@ -616,13 +629,12 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 if (key0 + kTileKeys > kv_end) {
                     const int at = pos + j, slot = at % S::kVSlots;
                     ok = ok && warp_wait(full0 + 8 * (S::kKSlots + slot), (at / S::kVSlots) & 1, gave_up);
-                    const int keep = kv_end - key0, part = (kTileKeys - keep) * 8;  // rows that stay; 16-byte pieces per half to clear
+                    const uint32_t tile = ring + (S::kKSlots + slot) * S::kKvBytes + (row & 7) * 16;
                     if (ok)
-                        for (int i = row; i < part * S::kHalves; i += 128) {
-                            const int hf = i >= part, r = i - hf * part;
-                            const uint32_t at_b = ring + (S::kKSlots + slot) * S::kKvBytes + hf * S::kKvHalf + keep * 128 + r * 16;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at_b), "r"(0) : "memory");
-                        }
+                        for (int r = kv_end - key0 + (row >> 3); r < kTileKeys; r += 16)
+#pragma unroll
+                            for (int hf = 0; hf < S::kHalves; ++hf)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + hf * S::kKvHalf + r * 128), "r"(0) : "memory");
                     fence_async_proxy();
                 }
                 fence_before_sync();
@@ -633,6 +645,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             if (!ok) break;
             done_other += s ? (steps + 1) / 2 : steps / 2;
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
+            if (m == -INFINITY) l = 0.0f;  // nothing seen: exp2_poly leaves 2^-126 each
             // every warp is through with the item before
             if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
             if (!wide) {  // maxima and sums of both streams
@@ -703,7 +716,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.o_free));
-            if (threadIdx.x == 0 && has_first && !has_last) ws.desc[cta] = SplitDesc{1, p.h, p.r0, p.tok0, p.n_tok, p.c_last, {0, 0}};
+            if (threadIdx.x == 0 && has_first && !has_last)
+                ws.desc[cta] = SplitDesc{1, p.h, p.r0, p.tok0, p.n_tok, share_owner(shares, sh.open_unit), {0, 0}};
             pos += n_tiles;
         }
     }
@@ -735,6 +749,25 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
                 const float* const o = ws.o + lane * kPerLane;
                 const bool mine = lane * kPerLane < a.head_dim;
                 float acc[kPerLane] = {}, l = 0.0f, m = -INFINITY;
+                float v[8][kPerLane];
+                auto fetch = [&](int i) {  // eight pieces' sums from piece i on
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+#pragma unroll
+                        for (int k = 0; k < kPerLane; ++k) v[u][k] = 0.0f;
+                        if (i + u < n && mine) {
+                            const float* q = o + slot(i + u) * DP;
+                            if constexpr (kPerLane == 4) {
+                                const float4 w = *reinterpret_cast<const float4*>(q);
+                                v[u][0] = w.x; v[u][1] = w.y; v[u][2] = w.z; v[u][3] = w.w;
+                            } else {
+                                const float2 w = *reinterpret_cast<const float2*>(q);
+                                v[u][0] = w.x; v[u][1] = w.y;
+                            }
+                        }
+                    }
+                };
+                fetch(0);  // while the maxima come in
                 for (int i0 = 0; i0 < n; i0 += 32) {  // 32 pieces at a time, rescaled to the largest maximum so far
                     const float2 ml = i0 + lane < n ? ws.ml[slot(i0 + lane)] : make_float2(-INFINITY, 0.0f);
                     float mx = ml.x;
@@ -751,24 +784,8 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
                     for (int k = 16; k; k >>= 1) li += __shfl_xor_sync(0xffffffffu, li, k);
                     l += li;
                     const int e = min(32, n - i0);
-                    for (int i = 0; i < e; i += 8) {  // eight loads in flight
-                        float v[8][kPerLane];
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            if (i + u < e && mine) {
-                                const float* q = o + slot(i0 + i + u) * DP;
-                                if constexpr (kPerLane == 4) {
-                                    const float4 w = *reinterpret_cast<const float4*>(q);
-                                    v[u][0] = w.x; v[u][1] = w.y; v[u][2] = w.z; v[u][3] = w.w;
-                                } else {
-                                    const float2 w = *reinterpret_cast<const float2*>(q);
-                                    v[u][0] = w.x; v[u][1] = w.y;
-                                }
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < kPerLane; ++k) v[u][k] = 0.0f;
-                            }
-                        }
+                    for (int i = 0; i < e; i += 8) {
+                        if (i0 + i > 0) fetch(i0 + i);
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
                             const float fi = __shfl_sync(0xffffffffu, f, (i + u) & 31);
