@@ -227,6 +227,7 @@ class Context:
         self.k_cap = k_cap
         self.hidden = hidden
         self.attn = None
+        self._geometry = (0, 0, 0, None)
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -433,71 +434,72 @@ class Context:
         c = make_attn_config(**cfg)
         self._check(self._lib.hvd_set_attention(self._h, C.byref(c)), "hvd_set_attention")
         self.attn = c
-        # the current stream's handle without a Stream object: these calls are made once per layer
+        # These calls are made once per layer: what they check against is kept as plain values, the current stream's handle is
+        # taken without a Stream object, and the rows' structs are filled anew by every call (the library reads them before it
+        # returns).
         self._raw_stream, self._dev = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device()
-        self._attn_type = torch.float16 if c.dtype == F16 else torch.bfloat16
-        # the calls' argument structs, filled anew by every call (the library reads them before it returns)
+        self._geometry = (c.n_q_heads, c.n_kv_heads, c.head_dim, torch.float16 if c.dtype == F16 else torch.bfloat16)
         self._arg = [HvdHeads() for _ in range(4)]
         self._arg_ref = [C.byref(h) for h in self._arg]
 
-    def _cache_arg(self, cache, what):
-        a = self.attn
-        if a is not None:
-            if cache.heads != (a.n_kv_heads, a.head_dim):
-                raise HvdError(f"{what}: the cache has other heads than hvd_set_attention was given")
-            if cache.type is not self._attn_type:
-                raise HvdError(f"{what}: the cache has another type than hvd_set_attention was given")
-        return cache._ref
-
-    def _heads_arg(self, i, t, heads, total_rows, what):
+    def _heads_arg(self, i, t, heads, total_rows):
         """Argument struct i for rows of heads: a tensor [total_rows or more, heads, head_dim] with contiguous heads."""
-        a = self.attn
-        if a is None:
-            return None      # the library says what is missing
+        _, _, d, dtype = self._geometry
+        if dtype is None:
+            return None      # hvd_set_attention is missing: the library says so
         shape = t.shape
-        if len(shape) != 3 or shape[0] < total_rows or shape[1] != heads or shape[2] != a.head_dim:
-            raise HvdError(f"{what}: a tensor [total_rows, {heads}, {a.head_dim}] (rows, n_q_heads or n_kv_heads, head_dim) is needed")
-        if t.dtype is not self._attn_type:
-            raise HvdError(f"{what}: another type than hvd_set_attention was given")
+        if len(shape) != 3 or shape[1] != heads or shape[2] != d or shape[0] < total_rows:
+            raise HvdError(f"a tensor [total_rows, {heads}, {d}] (rows, n_q_heads or n_kv_heads, head_dim) is needed, not {tuple(shape)}")
+        if t.dtype is not dtype:
+            raise HvdError("q, k, v and the outputs have another type than hvd_set_attention was given")
         row, head, e = t.stride()
-        if e != 1:
-            raise HvdError(f"{what}: the elements of a head must be contiguous")
+        if e != 1 and d > 1:
+            raise HvdError("the elements of a head must be contiguous")
         h = self._arg[i]
         h.p = t.data_ptr()
         # a dimension of length 1 may carry any stride
-        h.row_stride = row if shape[0] > 1 else shape[1] * a.head_dim
-        h.head_stride = head if shape[1] > 1 else a.head_dim
+        h.row_stride = row if shape[0] > 1 else heads * d
+        h.head_stride = head if heads > 1 else d
         return self._arg_ref[i]
 
-    def _head_counts(self):
-        a = self.attn
-        return (0, 0) if a is None else (a.n_q_heads, a.n_kv_heads)
+    def _cache_arg(self, cache):
+        """The cache's struct and the current stream, once the geometry is set (the library refuses the call otherwise)."""
+        if self.attn is None:
+            return cache._ref, None
+        _, nkv, d, dtype = self._geometry
+        if cache.heads != (nkv, d):
+            raise HvdError("the cache has other heads than hvd_set_attention was given")
+        if cache.type is not dtype:
+            raise HvdError("the cache has another type than hvd_set_attention was given")
+        return cache._ref, self._raw_stream(self._dev)
 
     def hvd_rope_append(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, k, v, q_out, status):
-        w = "hvd_rope_append"
-        nq, nkv = self._head_counts()
+        ref, stream = self._cache_arg(cache)
+        nq, nkv = self._geometry[:2]
         h = self._heads_arg
-        st = self._lib.hvd_rope_append(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform, total_rows,
-                                       _ptr(sel_len), _ptr(parent), h(0, q, nq, total_rows, w), h(1, k, nkv, total_rows, w),
-                                       h(2, v, nkv, total_rows, w), h(3, q_out, nq, total_rows, w), _ptr(status), self._raw_stream(self._dev) if self.attn is not None else None)
+        st = self._lib.hvd_rope_append(
+            self._h, B, ref, cache_len.data_ptr(), None if row_off is None else row_off.data_ptr(), k_uniform, total_rows,
+            None if sel_len is None else sel_len.data_ptr(), None if parent is None else parent.data_ptr(),
+            h(0, q, nq, total_rows), h(1, k, nkv, total_rows), h(2, v, nkv, total_rows), h(3, q_out, nq, total_rows),
+            status.data_ptr(), stream)
         if st:
-            self._check(st, w)
+            self._check(st, "hvd_rope_append")
 
     def hvd_attn_paged(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, out, lse=None,
                        status=None):
-        w = "hvd_attn_paged"
-        nq, _ = self._head_counts()
-        st = self._lib.hvd_attn_paged(self._h, B, self._cache_arg(cache, w), _ptr(cache_len), _ptr(row_off), k_uniform, total_rows,
-                                      _ptr(sel_len), _ptr(parent), self._heads_arg(0, q, nq, total_rows, w),
-                                      self._heads_arg(1, out, nq, total_rows, w), _ptr(lse), _ptr(status), self._raw_stream(self._dev) if self.attn is not None else None)
+        ref, stream = self._cache_arg(cache)
+        nq = self._geometry[0]
+        st = self._lib.hvd_attn_paged(
+            self._h, B, ref, cache_len.data_ptr(), None if row_off is None else row_off.data_ptr(), k_uniform, total_rows,
+            None if sel_len is None else sel_len.data_ptr(), None if parent is None else parent.data_ptr(),
+            self._heads_arg(0, q, nq, total_rows), self._heads_arg(1, out, nq, total_rows),
+            None if lse is None else lse.data_ptr(), None if status is None else status.data_ptr(), stream)
         if st:
-            self._check(st, w)
+            self._check(st, "hvd_attn_paged")
 
     def hvd_kv_commit(self, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
                       n_commit, new_len):
-        w = "hvd_kv_commit"
-        st = self._lib.hvd_kv_commit(self._h, B, self._cache_arg(cache, w), n_layers, layer_stride, _ptr(cache_len),
-                                     _ptr(parent), _ptr(sel_draft), _ptr(sel_len), _ptr(accepted), _ptr(committed),
-                                     _ptr(n_commit), _ptr(new_len), self._raw_stream(self._dev) if self.attn is not None else None)
-        if st:
-            self._check(st, w)
+        ref, stream = self._cache_arg(cache)
+        self._check(self._lib.hvd_kv_commit(self._h, B, ref, n_layers, layer_stride, _ptr(cache_len), _ptr(parent), _ptr(sel_draft),
+                                            _ptr(sel_len), _ptr(accepted), _ptr(committed), _ptr(n_commit), _ptr(new_len), stream),
+                    "hvd_kv_commit")

@@ -4,9 +4,10 @@
 // turns, so that t * w modulo one turn is an integer product that wraps: exact at every position, where a
 // 32-bit float product is off by thousandths of a radian from position 10^5 on.  The upper 32 bits go to sincospi.
 //
-// Bandwidth: every element is read once and written once.  A CTA takes a few tokens: their sines and cosines (the same
-// for all heads) are computed once into shared memory, then 16-byte vectors stream through, a thread keeping its
-// place inside the head and stepping over the heads, so that no index is divided in the loop.
+// Bandwidth: every element is read once and written once.  A CTA takes a few tokens.  Where a token goes hangs on four or five global
+// round trips (request, lengths, page), so the rows themselves, which hang on none, are asked for first and wait in registers;
+// the sines and cosines, the same for all heads, are computed once into shared memory.  A thread keeps its place inside
+// the head and steps over the heads, so that no index is divided in the loop.
 #include "hvd_attn.cuh"
 
 #include <cuda_bf16.h>
@@ -85,10 +86,43 @@ __device__ __forceinline__ void turn_pairs(uint4& x, const float2* cs, int n) {
     }
 }
 
-template <typename E, int LAYOUT>
+// Where a thread is among the heads of the CTA's tokens: q heads, k heads, v heads of the first token, then the next's.
+struct Place {
+    int t, h;
+    __device__ __forceinline__ Place(int at, int heads) : t(at / heads), h(at - (at / heads) * heads) {}
+    __device__ __forceinline__ void step(const Place& by, int heads) {
+        t += by.t;
+        h += by.h;
+        if (h >= heads) { h -= heads; ++t; }
+    }
+};
+
+template <typename E>
+__device__ __forceinline__ const E* source(const RopeArgs& a, int64_t row, int h) {
+    if (h < a.n_q_heads) return reinterpret_cast<const E*>(a.q.p) + row * a.q.row_stride + (int64_t)h * a.q.head_stride;
+    h -= a.n_q_heads;
+    if (h < a.n_kv_heads) return reinterpret_cast<const E*>(a.k.p) + row * a.k.row_stride + (int64_t)h * a.k.head_stride;
+    h -= a.n_kv_heads;
+    return reinterpret_cast<const E*>(a.v.p) + row * a.v.row_stride + (int64_t)h * a.v.head_stride;
+}
+
+// NULL: the token is not cached
+template <typename E>
+__device__ __forceinline__ E* target(const RopeArgs& a, const Token& tk, int h) {
+    if (h < a.n_q_heads) return reinterpret_cast<E*>(a.q_out.p) + tk.row * a.q_out.row_stride + (int64_t)h * a.q_out.head_stride;
+    h -= a.n_q_heads;
+    if (tk.kv < 0) return nullptr;
+    const bool is_v = h >= a.n_kv_heads;
+    return reinterpret_cast<E*>(is_v ? a.c.v : a.c.k) + tk.kv + (int64_t)(is_v ? h - a.n_kv_heads : h) * a.c.head_stride;
+}
+
+// WHOLE: rotated elements come in whole 16-byte vectors with their partners (always so for PAIRS; HALVES need rot_dim / 2 to be a
+// multiple of 8).
+template <typename E, int LAYOUT, bool WHOLE>
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArgs a, const int tokens_per_cta) {
     __shared__ Token tok[kRopeTokens];
     __shared__ __align__(16) float2 cs[kRopeTokens][HVD_MAX_HEAD_DIM / 2];
+    __shared__ unsigned long long turns[HVD_MAX_HEAD_DIM / 2];
     __shared__ int pos[kRopeTokens];
     const ChunkArgs& c = a.c;
     pdl_trigger();
@@ -107,37 +141,62 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
         return;
     }
     const int64_t first = (int64_t)blockIdx.x * tokens_per_cta;
+    const int n_tok = (int)min((int64_t)tokens_per_cta, c.total_rows - first);
+
+    // ---- a unit is a piece of a head: HALVES turn vector u with its partner half a rotation on, the rest are single vectors
+    const int D = a.head_dim, nvec = D / 8, half = a.rot_dim / 2, heads = a.n_q_heads + 2 * a.n_kv_heads;
+    const int n_turn = LAYOUT == HVD_ROPE_HALVES && WHOLE ? half / 8 : 0;
+    const int units = !WHOLE ? D - half : (LAYOUT == HVD_ROPE_PAIRS ? nvec : n_turn + (D - a.rot_dim) / 8);
+    const int per = (int)blockDim.x / units;  // heads side by side
+    const int u = (int)threadIdx.x % units, h0 = (int)threadIdx.x / units;
+    const bool mine = h0 < per, turned = u < n_turn;
+    const int e0 = turned || LAYOUT == HVD_ROPE_PAIRS ? 8 * u : a.rot_dim + 8 * (u - n_turn);  // first element of the (first) vector
+    constexpr int kAhead = LAYOUT == HVD_ROPE_PAIRS ? 8 : 4;
+    uint4 x[kAhead], y[kAhead];
+    Place get(h0, heads), put(h0, heads);
+    const Place stride(per, heads);
+    auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (mine && get.t < n_tok) {
+                const E* src = source<E>(a, first + get.t, get.h) + e0;
+                x[i] = *reinterpret_cast<const uint4*>(src);
+                if (turned) y[i] = *reinterpret_cast<const uint4*>(src + half);
+            }
+            get.step(stride, heads);
+        }
+    };
+    if (WHOLE) fetch();
+
+    for (int j = threadIdx.x; j < half; j += blockDim.x) turns[j] = a.turns[j];
     const int b0 = request_of(c, first);
-    if ((int)threadIdx.x < tokens_per_cta) {
+    if ((int)threadIdx.x < n_tok) {
         const int i = threadIdx.x;
         Token t = {first + i, -1, -1};
-        if (t.row < c.total_rows) {
-            int b = b0;
-            if (c.row_off) while (b + 1 < c.B && c.row_off[b + 1] <= t.row) ++b;
-            else b = (int)min(t.row / (c.k_uniform + 1), (int64_t)c.B);
-            if (b < c.B) {
-                const Chunk ch = load_chunk(c, b);
-                const int64_t at = t.row - ch.r0;
-                if (!ch.bad && at >= 0 && at < ch.n_new) {
-                    t.b = b;
-                    const int p = ch.base + (int)at;
-                    const int64_t page = page_of(c, b, p);
-                    if (page >= 0) t.kv = slot_offset(c, page, p);
-                    int depth = (int)at;
-                    unsigned long long nodes;
-                    if (c.parent) tree_line(c, b, (int)at, nodes, depth);
-                    pos[i] = ch.base + depth;
-                }
+        int b = b0;
+        if (c.row_off) while (b + 1 < c.B && c.row_off[b + 1] <= t.row) ++b;
+        else b = (int)min(t.row / (c.k_uniform + 1), (int64_t)c.B);
+        if (b < c.B) {
+            const Chunk ch = load_chunk(c, b);
+            const int64_t at = t.row - ch.r0;
+            if (!ch.bad && at >= 0 && at < ch.n_new) {
+                t.b = b;
+                const int p = ch.base + (int)at;
+                const int64_t page = page_of(c, b, p);
+                int depth = (int)at;
+                unsigned long long nodes;
+                if (c.parent) tree_line(c, b, (int)at, nodes, depth);
+                pos[i] = ch.base + depth;
+                if (page >= 0) t.kv = slot_offset(c, page, p);
             }
         }
         tok[i] = t;
     }
     __syncthreads();
-    const int half = a.rot_dim / 2;
-    for (int i = threadIdx.x; i < tokens_per_cta * half; i += blockDim.x) {
+    for (int i = threadIdx.x; i < n_tok * half; i += blockDim.x) {
         const int t = i / half, j = i - t * half;
         if (tok[t].b >= 0) {
-            const unsigned long long turn = (unsigned long long)pos[t] * a.turns[j];  // modulo one turn
+            const unsigned long long turn = (unsigned long long)pos[t] * turns[j];  // modulo one turn
             float s, co;
             sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s, &co);  // 2^-31: turns to half turns
             cs[t][j] = make_float2(co * a.magnitude, s * a.magnitude);
@@ -145,54 +204,40 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
     }
     __syncthreads();
 
-    const int D = a.head_dim, nvec = D / 8;
-    const bool whole = LAYOUT == HVD_ROPE_PAIRS || half % 8 == 0;  // pairs lie in whole 16-byte vectors
-    const int n_turned = a.n_q_heads + a.n_kv_heads;
-    for (int t = 0; t < tokens_per_cta; ++t) {
-        const Token tk = tok[t];
-        if (tk.b < 0) continue;
-        // queries and keys: `units` pieces per head
-        const int units = LAYOUT == HVD_ROPE_PAIRS ? nvec : (whole ? half / 8 + (D - a.rot_dim) / 8 : half + (D - a.rot_dim));
-        const int per = (int)blockDim.x / units;  // heads side by side
-        const int u = (int)threadIdx.x % units, h0 = (int)threadIdx.x / units;
-        for (int h = h0; h < n_turned && h0 < per; h += per) {
-            const bool isq = h < a.n_q_heads;
-            const int hk = h - a.n_q_heads;
-            if (!isq && tk.kv < 0) continue;
-            const E* src = isq ? reinterpret_cast<const E*>(a.q.p) + tk.row * a.q.row_stride + (int64_t)h * a.q.head_stride
-                               : reinterpret_cast<const E*>(a.k.p) + tk.row * a.k.row_stride + (int64_t)hk * a.k.head_stride;
-            E* dst = isq ? reinterpret_cast<E*>(a.q_out.p) + tk.row * a.q_out.row_stride + (int64_t)h * a.q_out.head_stride
-                         : reinterpret_cast<E*>(c.k) + tk.kv + (int64_t)hk * c.head_stride;
-            if (LAYOUT == HVD_ROPE_PAIRS) {
-                uint4 x = *reinterpret_cast<const uint4*>(src + 8 * u);
-                turn_pairs<E>(x, &cs[t][min(4 * u, HVD_MAX_HEAD_DIM / 2 - 4)], half - 4 * u);
-                *reinterpret_cast<uint4*>(dst + 8 * u) = x;
-            } else if (whole) {
-                if (u < half / 8) {
-                    uint4 x = *reinterpret_cast<const uint4*>(src + 8 * u);
-                    uint4 y = *reinterpret_cast<const uint4*>(src + half + 8 * u);
-                    turn_halves<E>(x, y, &cs[t][8 * u]);
-                    *reinterpret_cast<uint4*>(dst + 8 * u) = x;
-                    *reinterpret_cast<uint4*>(dst + half + 8 * u) = y;
-                } else {
-                    const int e = a.rot_dim + 8 * (u - half / 8);
-                    *reinterpret_cast<uint4*>(dst + e) = *reinterpret_cast<const uint4*>(src + e);
+    if (WHOLE) {
+        while (mine && put.t < n_tok) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (put.t < n_tok) {
+                    const Token tk = tok[put.t];
+                    E* dst = tk.b >= 0 ? target<E>(a, tk, put.h) : nullptr;
+                    if (dst) {
+                        if (put.h < a.n_q_heads + a.n_kv_heads) {
+                            if (LAYOUT == HVD_ROPE_PAIRS) turn_pairs<E>(x[i], &cs[put.t][min(4 * u, HVD_MAX_HEAD_DIM / 2 - 4)], half - 4 * u);
+                            else if (turned) turn_halves<E>(x[i], y[i], &cs[put.t][8 * u]);
+                        }
+                        *reinterpret_cast<uint4*>(dst + e0) = x[i];
+                        if (turned) *reinterpret_cast<uint4*>(dst + e0 + half) = y[i];
+                    }
                 }
-            } else if (u < half) {
-                const float x = widen(src[u]), y = widen(src[u + half]);
-                dst[u] = (E)(x * cs[t][u].x - y * cs[t][u].y);
-                dst[u + half] = (E)(x * cs[t][u].y + y * cs[t][u].x);
-            } else {
-                const int e = a.rot_dim + u - half;
-                dst[e] = src[e];
+                put.step(stride, heads);
             }
+            if (put.t < n_tok) fetch();
         }
-        if (tk.kv >= 0) {  // values
-            const int perv = (int)blockDim.x / nvec, uv = (int)threadIdx.x % nvec, hv = (int)threadIdx.x / nvec;
-            for (int h = hv; h < a.n_kv_heads && hv < perv; h += perv) {
-                const E* src = reinterpret_cast<const E*>(a.v.p) + tk.row * a.v.row_stride + (int64_t)h * a.v.head_stride;
-                E* dst = reinterpret_cast<E*>(c.v) + tk.kv + (int64_t)h * c.head_stride;
-                *reinterpret_cast<uint4*>(dst + 8 * uv) = *reinterpret_cast<const uint4*>(src + 8 * uv);
+    } else {  // element by element: u < half an element and its partner, then single ones
+        for (; mine && put.t < n_tok; put.step(stride, heads)) {
+            const Token tk = tok[put.t];
+            E* dst = tk.b >= 0 ? target<E>(a, tk, put.h) : nullptr;
+            if (!dst) continue;
+            const E* src = source<E>(a, tk.row, put.h);
+            if (u < half) {
+                const E x0 = src[u], y0 = src[u + half];
+                const bool turn = put.h < a.n_q_heads + a.n_kv_heads;
+                const float2 f = cs[put.t][u];
+                dst[u] = turn ? (E)(widen(x0) * f.x - widen(y0) * f.y) : x0;
+                dst[u + half] = turn ? (E)(widen(x0) * f.y + widen(y0) * f.x) : y0;
+            } else {
+                dst[u + half] = src[u + half];  // rot_dim + (u - half)
             }
         }
     }
@@ -204,10 +249,14 @@ hvd_status launch_rope_append(hvd_ctx* ctx, const RopeArgs& a, bool f16, int lay
     const int tpc = a.c.total_rows > 4LL * ctx->num_sms ? kRopeTokens : 1;
     const int64_t grid = (a.c.total_rows + tpc - 1) / tpc + (a.c.B + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
     const bool pdl = (ctx->pdl_mask & 16) != 0;
+    const bool whole = a.rot_dim % 16 == 0;
     auto run = [&](auto kernel) { return launch_kernel(pdl, kernel, dim3((unsigned)grid), dim3(kRopeThreads), 0, stream, a, tpc); };
-    cudaError_t e;
-    if (f16) e = layout == HVD_ROPE_PAIRS ? run(rope_append_kernel<__half, HVD_ROPE_PAIRS>) : run(rope_append_kernel<__half, HVD_ROPE_HALVES>);
-    else e = layout == HVD_ROPE_PAIRS ? run(rope_append_kernel<__nv_bfloat16, HVD_ROPE_PAIRS>) : run(rope_append_kernel<__nv_bfloat16, HVD_ROPE_HALVES>);
+    auto pick = [&](auto e) {
+        using E = decltype(e);
+        if (layout == HVD_ROPE_PAIRS) return run(rope_append_kernel<E, HVD_ROPE_PAIRS, true>);
+        return whole ? run(rope_append_kernel<E, HVD_ROPE_HALVES, true>) : run(rope_append_kernel<E, HVD_ROPE_HALVES, false>);
+    };
+    const cudaError_t e = f16 ? pick(__half()) : pick(__nv_bfloat16());
     return e == cudaSuccess ? HVD_OK : cuda_fail(ctx, e, "rope_append_kernel");
 }
 
