@@ -607,7 +607,7 @@ enum { HVD_MAX_HEAD_DIM = 128, HVD_MAX_HEAD_GROUP = 128 };
 
 typedef struct {
     int32_t n_q_heads;     /* a multiple of n_kv_heads, at most HVD_MAX_HEAD_GROUP times as many */
-    int32_t n_kv_heads;    /* >= 1; query head h reads key/value head h / (n_q_heads / n_kv_heads) */
+    int32_t n_kv_heads;    /* 1 .. 4096; query head h reads key/value head h / (n_q_heads / n_kv_heads) */
     int32_t head_dim;      /* a multiple of 8, 8 .. HVD_MAX_HEAD_DIM */
     int32_t dtype;         /* HVD_BF16 or HVD_F16: q, k, v, out and the cache */
     float softmax_scale;   /* > 0; 0 stands for 1 / sqrt(head_dim) */
@@ -697,7 +697,8 @@ HVD_API hvd_status hvd_attn_paged(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* c
  * lowest index that carries the next token of `committed`.  Where the path ends early (outputs of another
  * call) or an entry of the page table lies outside the pool, the rest of the request's nodes stays where it is.
  *
- * cache        the first layer's; layer l's arrays start l * layer_stride elements (a multiple of 8) further on
+ * cache        the first layer's; layer l's arrays start l * layer_stride elements (a multiple of 8) further on,
+ *              n_layers 1 .. 4096
  * sel_draft, parent int32 [B, k_cap]; sel_len, accepted, n_commit int32 [B]; committed int32 [B, k_cap + 1]:
  *              hvd_verify_commit_tree's arguments and outputs.  Chain: parent = NULL, and sel_draft, sel_len,
  *              accepted and committed may be NULL; nothing is moved

@@ -13,7 +13,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 const char* config_fault(const hvd_attn_config& c) {
     if (c.n_kv_heads < 1 || c.n_q_heads < 1 || c.n_q_heads % c.n_kv_heads != 0) return "n_q_heads must be a multiple of n_kv_heads >= 1";
     if (c.n_q_heads / c.n_kv_heads > HVD_MAX_HEAD_GROUP) return "more than HVD_MAX_HEAD_GROUP query heads per key/value head";
-    if (c.n_kv_heads > 65535) return "n_kv_heads above 65535";
+    if (c.n_kv_heads > 4096) return "n_kv_heads above 4096";
     if (c.head_dim < 8 || c.head_dim > HVD_MAX_HEAD_DIM || c.head_dim % 8 != 0) return "head_dim must be a multiple of 8 in [8, HVD_MAX_HEAD_DIM]";
     if (c.dtype != HVD_BF16 && c.dtype != HVD_F16) return "dtype must be HVD_BF16 or HVD_F16";
     if (!(c.softmax_scale >= 0.0f) || isinf(c.softmax_scale)) return "softmax_scale must be finite and >= 0";
@@ -210,14 +210,14 @@ hvd_status hvd_kv_commit(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int
     if (const char* w = cache_fault(ctx, B, cache, cache_len)) return fail_at(ctx, HVD_ERR_INVALID_ARG, who, w);
     if (!n_commit || !new_len || (parent && (!sel_draft || !sel_len || !accepted || !committed)))
         return fail_at(ctx, HVD_ERR_INVALID_ARG, who, "NULL pointer");
-    if (n_layers < 1 || n_layers > 65535) return fail_at(ctx, HVD_ERR_INVALID_ARG, who, "n_layers outside [1, 65535]");
+    if (n_layers < 1 || n_layers > 4096) return fail_at(ctx, HVD_ERR_INVALID_ARG, who, "n_layers outside [1, 4096]");
     if (layer_stride % 8 != 0 || (n_layers > 1 && layer_stride <= 0))
         return fail_at(ctx, HVD_ERR_INVALID_ARG, who, "layer_stride must be a positive multiple of 8");
     KvCommitArgs a = {};
     a.c = chunk_args(ctx, B, *cache, cache_len, nullptr, 0, 0, sel_len, parent);
     a.n_layers = n_layers; a.n_kv_heads = ctx->attn.n_kv_heads; a.head_dim = ctx->attn.head_dim;
     a.layer_stride = layer_stride;
-    a.sel_draft = sel_draft; a.accepted = accepted; a.committed = committed; a.n_commit = n_commit; a.new_len = new_len;
+    a.sel_draft = sel_draft; a.accepted = accepted; a.committed = committed; a.n_commit = n_commit; a.new_len = new_len; a.in_place = new_len == cache_len;
     a.arrived = ctx->at_arrived;
     return launch_kv_commit(ctx, a, static_cast<cudaStream_t>(stream));
 }

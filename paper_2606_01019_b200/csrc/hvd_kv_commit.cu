@@ -15,39 +15,41 @@ constexpr uint32_t kFull = 0xffffffffu;
 
 __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArgs a) {
     __shared__ int64_t from[kTreeRows], to[kTreeRows];
-    __shared__ int n_moves;
+    __shared__ int n_moves, new_length;
     const ChunkArgs& c = a.c;
     const int b = blockIdx.x;
     pdl_trigger();
     pdl_wait();
+    const int kc = c.k_cap;
     if (threadIdx.x < 32) {
         const int lane = threadIdx.x;
+        // all loads that hang on nothing at once
         const int base = c.cache_len[b];
         const int w = a.n_commit[b];
-        const bool usable = w > 0 && base >= 0 && (int64_t)base + w <= (int64_t)c.table_stride * c.page_size;
-        if (lane == 0) {
-            // new_len may be cache_len: it is written once every CTA of the request has read the old length
-            __threadfence();
-            const uint32_t n = atomicAdd(&a.arrived[b], 1u);
-            if (n + 1 == gridDim.y) {
-                a.arrived[b] = 0u;  // zero at rest
-                a.new_len[b] = usable ? base + w : base;
-            }
-        }
-        int moves = 0;
-        if (usable && c.parent) {
-            const int kc = c.k_cap;
-            const int m = max(0, min(c.sel_len[b], kc));
-            const int most = min(min(a.accepted[b], w - 1), m);
-            const int32_t* z = a.committed + (int64_t)b * (kc + 1);
-            int dt[2], pr[2], zt[2];
+        int m = 0, most = 0, dt[2] = {-1, -1}, pr[2] = {-2, -2}, zt[2] = {-1, -1};
+        if (c.parent) {
+            m = c.sel_len[b];
+            most = a.accepted[b];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {  // nodes lane, lane + 32
                 const int i = lane + 32 * k;
-                dt[k] = i < m ? a.sel_draft[(int64_t)b * kc + i] : -1;
-                pr[k] = i < m ? c.parent[(int64_t)b * kc + i] : -2;
-                zt[k] = i < kc ? z[i] : -1;
+                if (i < kc) {
+                    dt[k] = a.sel_draft[(int64_t)b * kc + i];
+                    pr[k] = c.parent[(int64_t)b * kc + i];
+                    zt[k] = a.committed[(int64_t)b * (kc + 1) + i];
+                }
             }
+            m = max(0, min(m, kc));
+            most = min(min(most, w - 1), m);
+        }
+        const bool usable = w > 0 && base >= 0 && (int64_t)base + w <= (int64_t)c.table_stride * c.page_size;
+        const int len = usable ? base + w : base;
+        if (lane == 0) {
+            new_length = len;
+            if (!a.in_place && blockIdx.y == 0) a.new_len[b] = len;
+        }
+        int moves = 0;
+        if (usable && c.parent) {
             int cur = -1;
             int src[2] = {-1, -1};  // lane holds the nodes of steps lane, lane + 32
             int steps = 0;
@@ -87,24 +89,30 @@ __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArg
     }
     __syncthreads();
     const int n = n_moves;
-    if (n == 0) return;
     const int nvec = a.head_dim / 8, heads = a.n_kv_heads;
-    const int64_t total = (int64_t)a.n_layers * 2 * heads * nvec;
-    for (int64_t w = (int64_t)blockIdx.y * kKvThreads + threadIdx.x; w < total; w += (int64_t)gridDim.y * kKvThreads) {
-        const int e = (int)(w % nvec);
-        const int64_t r = w / nvec;
-        const int h = (int)(r % heads);
-        const int64_t l2 = r / heads;  // layer * 2 + (key or value)
-        char* pool = (l2 & 1) ? c.v : c.k;
-        const int64_t col = (l2 >> 1) * a.layer_stride + (int64_t)h * c.head_stride + 8 * e;
-        for (int j = 0; j < n; j += 8) {
-            uint4 x[8];
+    const int total = a.n_layers * 2 * heads * nvec;  // below 2^30 by the limits on layers and heads
+    if (n > 0)
+        for (int w = blockIdx.y * kKvThreads + threadIdx.x; w < total; w += gridDim.y * kKvThreads) {
+            const int r = w / nvec, e = w - r * nvec;
+            const int l2 = r / heads, h = r - l2 * heads;  // l2: layer * 2 + (key or value)
+            char* pool = (l2 & 1) ? c.v : c.k;
+            const int64_t col = (int64_t)(l2 >> 1) * a.layer_stride + (int64_t)h * c.head_stride + 8 * e;
+            for (int j = 0; j < n; j += 8) {
+                uint4 x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j + i < n) x[i] = *reinterpret_cast<const uint4*>(pool + 2 * (col + from[j + i]));
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < n) x[i] = *reinterpret_cast<const uint4*>(pool + 2 * (col + from[j + i]));
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j + i < n) *reinterpret_cast<uint4*>(pool + 2 * (col + to[j + i])) = x[i];
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < n) *reinterpret_cast<uint4*>(pool + 2 * (col + to[j + i])) = x[i];
+            }
+        }
+    if (a.in_place && threadIdx.x == 0) {
+        // new_len is cache_len: it is written once every CTA of the request has read the old length
+        __threadfence();
+        if (atomicAdd(&a.arrived[b], 1u) + 1 == gridDim.y) {
+            a.arrived[b] = 0u;  // zero at rest
+            a.new_len[b] = new_length;
         }
     }
 }
