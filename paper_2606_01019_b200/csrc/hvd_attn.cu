@@ -407,16 +407,20 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 auto load_q = [&](bool ahead) {
                     if (ahead != (items == 0)) return true;
                     if (!warp_wait(smem_addr(&sh.q_empty), (items & 1) ^ 1, gave_up)) return false;
-                    const int n0 = (min(g.tile_tok, p.n_tok) + box_tok - 1) / box_tok;
-                    const int n1 = p.n_tok > g.tile_tok ? (p.n_tok - g.tile_tok + box_tok - 1) / box_tok : 0;
-                    if (lane == 0) mbar_expect(smem_addr(&sh.q_full), (uint32_t)((n0 + n1) * box_tok * a.group * 128 * S::kHalves));
+                    // Boxes behind the item's tokens lie outside the tensor and bring zeros: rows of zeros make scores and weights of
+                    // zero, which cost the tensor cores less power than what the shared memory held (ragged decode, in a long run,
+                    // 590 -> 549 us).
+                    const int nb = g.tile_tok / box_tok;  // boxes of a row tile
+                    const int n_box_q = p.n_tok > g.tile_tok ? 2 * nb : nb;
+                    if (lane == 0) mbar_expect(smem_addr(&sh.q_full), (uint32_t)(n_box_q * box_tok * a.group * 128 * S::kHalves));
                     __syncwarp();
-                    for (int x = lane; x < n0 + n1; x += 32) {
-                        const int t = x >= n0, bx = x - (t ? n0 : 0);
+                    for (int x = lane; x < n_box_q; x += 32) {
+                        const int t = x >= nb, bx = x - (t ? nb : 0), tok = t * g.tile_tok + bx * box_tok;
                         const uint32_t dst = tiles + t * S::kQBytes + bx * box_tok * a.group * 128;
+                        const int row = tok < p.n_tok ? p.r0 + p.tok0 + tok : (int)a.c.total_rows;
 #pragma unroll
                         for (int hf = 0; hf < S::kHalves; ++hf)
-                            tma_load_4d(dst + hf * S::kQHalf, &map_q, smem_addr(&sh.q_full), hf * 64, 0, p.r0 + p.tok0 + t * g.tile_tok + bx * box_tok, p.h);
+                            tma_load_4d(dst + hf * S::kQHalf, &map_q, smem_addr(&sh.q_full), hf * 64, 0, row, p.h);
                     }
                     return true;
                 };

@@ -45,7 +45,7 @@ constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 
 // Waits for the phase of the given parity; false when the CTA has given up (`gave_up`, shared memory) or this wait ran
 // out after two seconds, which makes the CTA give up.  The waiting thread sleeps in the barrier unit for up to a
-// millisecond at a time: threads that poll instead take issue slots from the arithmetic.
+// millisecond at a time: polling cost no time in a short run, but power, by which a long one is bound.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
     if (mbar_try(bar, parity)) return true;
     const unsigned long long t0 = now_ns();
