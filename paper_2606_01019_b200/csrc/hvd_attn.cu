@@ -187,9 +187,10 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
 }
 
 // w = exp2(x * scale - m) of a row's 64 scores, rounded to the cache's type and packed, into tensor memory over the scores; returns
-// their sums before rounding.  Every third pair goes through exp2_poly, which relieves the special function unit (two
-// row tiles of 32 K keys, us: none 96.5, every 8th 93.6, 4th 92.7, 3rd 91.6, 2nd 94.4).  That makes 2^-126 of a score of -infinity:
-// where there are some (`edge`) those weights are cleared by `seen`.
+// their sums before rounding.  Every eighth pair goes through exp2_poly, which relieves the special function unit but takes more power,
+// by which long runs are bound (2047 rows behind 1.5 to 9 K tokens, long runs, us: none 823, every 8th pair 791, 5th 811, 3rd 837,
+// 2nd 862; short runs are fastest with every 3rd).  That makes 2^-126 of a score of -infinity: where there are some (`edge`) those
+// weights are cleared by `seen`.
 template <typename E>
 __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t dst, float2 scale2, float m, bool edge, unsigned long long seen) {
     const float shift = m == -INFINITY ? 0.0f : -m;
@@ -201,7 +202,7 @@ __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t d
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             float2 e = fma2(make_float2(__uint_as_float(x[i][2 * k]), __uint_as_float(x[i][2 * k + 1])), scale2, shift2);
-            if (k % 3 == 2) e = exp2_poly(e);
+            if (k % 8 == 7) e = exp2_poly(e);
             else e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
             sum[k & 1] = add2(sum[k & 1], e);
             w[k] = pack2<E>(e.x, e.y);
@@ -209,7 +210,7 @@ __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t d
         if (edge) {
             const uint32_t bits = (uint32_t)(seen >> (32 * i));
 #pragma unroll
-            for (int k = 2; k < 16; k += 3) w[k] &= (((bits >> (2 * k)) & 1u) ? 0xffffu : 0u) | (((bits >> (2 * k + 1)) & 1u) ? 0xffff0000u : 0u);
+            for (int k = 7; k < 16; k += 8) w[k] &= (((bits >> (2 * k)) & 1u) ? 0xffffu : 0u) | (((bits >> (2 * k + 1)) & 1u) ? 0xffff0000u : 0u);
         }
         tmem_st16(dst + 16 * i, w);
     }
