@@ -557,7 +557,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             const int kv_end = p.base + p.tok0 + p.n_tok;
             const int n_rows = min(g.tile_tok, p.tok0 + p.n_tok - tok0) * a.group;
             const int tok = tok0 + row / a.group, grp = row % a.group;
-            const bool valid = row < n_rows, active = (row & ~31) < n_rows;
+            const bool valid = row < n_rows && HVD_IN_BOUNDS(a.c.dev_error, (int64_t)p.r0 + tok, 0, a.c.total_rows), active = (row & ~31) < n_rows;
             // what the row sees: keys below `upto`, in a tree also the nodes on its line
             unsigned long long nodes = 0ull;
             int upto = p.base + tok + 1;
@@ -801,6 +801,7 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
                 }
                 const int64_t row = d.r0 + d.tok0 + t;
                 const int head = d.h * a.group + grp;
+                if (!HVD_IN_BOUNDS(a.c.dev_error, row, 0, a.c.total_rows)) continue;
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
                 if (mine) {
                     uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<E*>(a.out.p) + row * a.out.row_stride + (int64_t)head * a.out.head_stride + lane * kPerLane);
@@ -811,17 +812,23 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
             }
         }
     }
-    // requests: status, rows that are no new token
-    const int who = blockIdx.y * gridDim.x + blockIdx.x, n_who = gridDim.x * gridDim.y;
-    for (int b = who * (kFinishThreads / 32) + warp; b < a.c.B; b += n_who * (kFinishThreads / 32)) {
+    // requests: status, rows that are no new token (with drafts shorter than their rows most of the batch), several warps a request
+    const int n_warp = gridDim.x * gridDim.y * (kFinishThreads / 32), me = (blockIdx.y * gridDim.x + blockIdx.x) * (kFinishThreads / 32) + warp;
+    const int share = max(1, n_warp / a.c.B), nvec = a.head_dim / 8;
+    for (int64_t x = me; x < (int64_t)a.c.B * share; x += n_warp) {
+        const int b = (int)(x % a.c.B), s = (int)(x / a.c.B);
         const Chunk c = load_chunk(a.c, b);
-        if (a.status && lane == 0) a.status[b] = c.bad ? HVD_REQ_BAD_LEN : HVD_REQ_OK;
-        for (int i = c.n_new; i < c.rows; ++i)
-            for (int h = 0; h < a.n_q_heads; ++h) {
-                E* out = reinterpret_cast<E*>(a.out.p) + (c.r0 + i) * a.out.row_stride + (int64_t)h * a.out.head_stride;
-                if (8 * lane < a.head_dim) *reinterpret_cast<uint4*>(out + 8 * lane) = make_uint4(0u, 0u, 0u, 0u);
-                if (a.lse && lane == 0) a.lse[(c.r0 + i) * a.n_q_heads + h] = -INFINITY;
+        if (a.status && s == 0 && lane == 0) a.status[b] = c.bad ? HVD_REQ_BAD_LEN : HVD_REQ_OK;
+        for (int64_t i = (int64_t)c.n_new + s; i < c.rows; i += share) {
+            const int64_t row = c.r0 + i;
+            if (!HVD_IN_BOUNDS(a.c.dev_error, row, 0, a.c.total_rows)) continue;
+            for (int v = lane; v < a.n_q_heads * nvec; v += 32) {
+                const int h = v / nvec, e = v - h * nvec;
+                *reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.out.p) + row * a.out.row_stride + (int64_t)h * a.out.head_stride + 8 * e) = make_uint4(0u, 0u, 0u, 0u);
             }
+            if (a.lse)
+                for (int h = lane; h < a.n_q_heads; h += 32) a.lse[row * a.n_q_heads + h] = -INFINITY;
+        }
     }
 }
 

@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
                 unsigned long long nodes;
                 if (c.parent) tree_line(c, b, (int)at, nodes, depth);
                 pos[i] = ch.base + depth;
-                if (page >= 0) t.kv = slot_offset(c, page, p);
+                if (page >= 0 && HVD_IN_BOUNDS(c.dev_error, t.row, 0, c.total_rows)) t.kv = slot_offset(c, page, p);
             }
         }
         tok[i] = t;

@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from .binding import BF16, F32, STATE_DTYPE, Context
+from .binding import BF16, F32, STATE_DTYPE, Context, KvCache
 
 
 class DeviceBatch:
@@ -143,3 +143,37 @@ class DeviceBatch:
         out["target_tok"] = out["target_tok"][:self.total_rows]
         out["state"] = self.state.cpu().numpy().reshape(-1).view(STATE_DTYPE)
         return out
+
+
+class PagedCache:
+    """The target model's key/value cache for one batch: pools of pages for every layer, the page table, the cached
+    lengths, and the three calls of a target forward that work on it.  Every request gets pages for max_len tokens at
+    once; a serving engine hands them out as they are needed and only changes the table."""
+
+    def __init__(self, ctx: Context, *, B, n_layers, max_len, n_q_heads, n_kv_heads, head_dim, page_size=64, dtype=BF16, device="cuda",
+                 **attention):
+        import torch
+        ctx.hvd_set_attention(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype, **attention)
+        self.ctx, self.B, self.n_layers = ctx, B, n_layers
+        per = -(-max_len // page_size)
+        t = torch.bfloat16 if dtype == BF16 else torch.float16
+        self.k = torch.empty(n_layers, B * per, page_size, n_kv_heads, head_dim, dtype=t, device=device)
+        self.v = torch.empty_like(self.k)
+        self.table = torch.arange(B * per, dtype=torch.int32, device=device).reshape(B, per)
+        self.length = torch.zeros(B, dtype=torch.int32, device=device)     # tokens cached
+        self.status = torch.zeros(B, dtype=torch.int32, device=device)
+        self.layer = [KvCache(self.k[i], self.v[i], self.table) for i in range(n_layers)]
+
+    def append(self, layer, q, k, v, q_out, *, row_off=None, k_uniform=0, sel_len=None, parent=None):
+        """Rotates the new tokens' q (into q_out) and k, and caches k and v."""
+        self.ctx.hvd_rope_append(self.B, self.layer[layer], self.length, row_off, k_uniform, q.shape[0], sel_len, parent, q, k, v,
+                                 q_out, self.status)
+
+    def attend(self, layer, q, out, *, row_off=None, k_uniform=0, sel_len=None, parent=None, lse=None):
+        """Attention of the chunk's rows over the cache, which holds the chunk."""
+        self.ctx.hvd_attn_paged(self.B, self.layer[layer], self.length, row_off, k_uniform, q.shape[0], sel_len, parent, q, out, lse)
+
+    def commit(self, n_commit, *, sel_draft=None, sel_len=None, parent=None, accepted=None, committed=None):
+        """Takes the chunk's first n_commit tokens (of a tree: the root and its accepted nodes) into the cache."""
+        self.ctx.hvd_kv_commit(self.B, self.layer[0], self.n_layers, self.k.stride(0), self.length, parent, sel_draft, sel_len,
+                               accepted, committed, n_commit, self.length)

@@ -70,6 +70,17 @@ def test_rows_from_k_uniform_and_ragged_selection():
         assert (out[r] == 0).all() and torch.isinf(lse[r]).all()
 
 
+def test_many_rows_that_are_no_new_token():
+    """Short drafts in wide blocks of rows, as a ragged batch has them: the other rows come out as zeros."""
+    rng = np.random.default_rng(4)
+    B = 200
+    p = R.Problem(lens=[int(x) for x in rng.integers(0, 90, B)], rows=[33] * B, sel=[int(x) for x in rng.integers(-1, 4, B)], hq=5, hkv=1, d=80,
+                  page=16, seed=4)
+    out, lse = check(p)
+    rest = np.concatenate([np.arange(p.off[b] + p.n_new[b], p.off[b + 1]) for b in range(B)])
+    assert (out[rest] == 0).all() and torch.isinf(lse[rest]).all()
+
+
 def test_empty_requests_and_an_empty_batch():
     check(R.Problem(lens=[10, 0, 50, 3], rows=[0, 0, 4, 0], hq=4, hkv=2, d=64, page=16))
     p = R.Problem(lens=[10, 0], rows=[0, 0], hq=4, hkv=2, d=64, page=16)
@@ -288,3 +299,26 @@ def test_refusals():
     ctx.hvd_attn_paged(*args())
     R.check_attention(p, out, lse, R.attention(p))
     ctx.close()
+
+
+def _again(env, select):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    cmd = [sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "tests/test_gpu_attention.py", "tests/test_gpu_rope.py",
+           "tests/test_gpu_kv_commit.py", "tests/test_gpu_target_forward.py", "-k", select]
+    res = subprocess.run(cmd, cwd=root, env=dict(os.environ, **env), capture_output=True, text=True, timeout=900)
+    assert res.returncode == 0, res.stdout[-3000:] + res.stderr[-2000:]
+    assert " passed" in res.stdout
+
+
+def test_again_with_plain_launches():
+    """No programmatic dependent launch: results must not depend on how far consecutive kernels overlap."""
+    _again({"HVD_PDL_MASK": "0"}, "(random or trees or few_requests or decoding or rows or become) and not again")
+
+
+def test_again_against_the_bounds_checked_build():
+    """The build with -DHVD_DEBUG_BOUNDS: every context must close with device status 0."""
+    from paper_2606_01019_b200 import build
+    _again({"HVD_B200_LIB": build.build_bounds_checked(), "HVD_ASSERT_DEVICE_STATUS": "1"}, "not again")
