@@ -673,8 +673,8 @@ HVD_API hvd_status hvd_rope_append(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* 
  *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j)
  * Scores, statistics and sums are in 32 bits; the weights exp(x_j - running maximum) are rounded to the cache's
  * type for the product with v.  Rows that see nothing (rows beyond n_new, unreachable nodes, skipped
- * requests) get out = 0 and lse = -inf; rows of no request are not written.  Slots at and behind cache_len + n_new may hold anything, also NaN.  The
- * k and v of tokens below that have to be finite: a row's zero weight times an infinite v is NaN.
+ * requests) get out = 0 and lse = -inf; rows of no request are not written.  Slots at and behind cache_len + n_new may hold
+ * anything, also NaN, and so may tokens of the chunk for the rows that do not see them.
  * A page entry outside [0, n_pages) stands for a page of zeros.
  *
  * q    HOST struct, [total_rows] rows of n_q_heads heads

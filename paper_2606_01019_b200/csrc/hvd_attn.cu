@@ -68,10 +68,12 @@ struct Shared {  // behind the tiles
     uint64_t o_full[2][2];                       // [stream][buffer] a step's product with V is done
     uint64_t stats, o_free;                      // maxima and sums of both streams exchanged; the item's sums are read
     uint64_t piece_full[kPieces], piece_empty[kPieces];
+    uint64_t landed;                             // a V tile that is cleaned before it is full
     uint64_t drain;
     Piece piece[kPieces];
     uint32_t tmem;
     int gave_up;
+    int not_finite;       // some value of a chunk's own tokens was infinite or NaN
     struct { int b, h, qt, kv, r0, n_new, base; } start;  // where the CTA's share begins
     long long start_left;
     long long open_unit;  // of the item that the share leaves unfinished: its last tile's first unit
@@ -91,6 +93,7 @@ struct Work {
     SplitDesc* desc;   // [CTAs]
     float* o;          // [CTAs][2][256][DP]
     float2* ml;        // [CTAs][2][256] maximum (log2 units), sum
+    int* spare;        // some row is no new token
 };
 
 // ---------------------------------------------------------------- items
@@ -217,6 +220,25 @@ __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t d
     return add2(sum[0], sum[1]);
 }
 
+// Infinities and NaN that were cleared from the values of tokens [lo, hi), back into a row that sees them: columns [c0, c1) of its
+// output, or of its partial sums.  (Any positive weight times such a value is that value.)
+template <typename E>
+__device__ __noinline__ void restore_cleared(const AttnArgs& a, int b, int h, int lo, int hi, int upto, unsigned long long nodes, int node0, int c0, int c1,
+                                             E* out, float* part) {
+    for (int t = lo; t < hi; ++t) {
+        if (!(t < upto || (a.c.parent && ((nodes >> (t - node0)) & 1ull)))) continue;
+        const int64_t page = page_of(a.c, b, t);
+        if (page < 0) continue;
+        const E* val = reinterpret_cast<const E*>(a.c.v) + slot_offset(a.c, page, t) + (int64_t)h * a.c.head_stride;
+        for (int c = c0; c < c1; ++c) {
+            const float e = (float)val[c];
+            if (isfinite(e)) continue;
+            if (out) out[c] = (E)((float)out[c] + e);
+            else part[c] += e;
+        }
+    }
+}
+
 template <typename E, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int box_keys, const int box_tok, const __grid_constant__ CUtensorMap map_q,
@@ -241,8 +263,10 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             mbar_init(smem_addr(&sh.q_empty), 2);
             mbar_init(smem_addr(&sh.stats), kSoftmaxWarps);
             mbar_init(smem_addr(&sh.o_free), kSoftmaxWarps);
+            mbar_init(smem_addr(&sh.landed), 1);
             mbar_init(smem_addr(&sh.drain), 2);
             sh.gave_up = 0;
+            sh.not_finite = 0;
         }
         mbar_init_fence();
     }
@@ -253,11 +277,12 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     const int b0 = min(a.c.B, (int)threadIdx.x * per), b1 = min(a.c.B, b0 + per);
     long long mine = 0;
     Chunk c0 = {};
-    bool any_wide = false;
+    bool any_wide = false, spare = false;
     for (int b = b0; b < b1; ++b) {
         const Chunk c = load_chunk(a.c, b);
         if (b == b0) c0 = c;
         any_wide = any_wide || c.n_new > g.tile_tok;
+        spare = spare || c.rows > c.n_new;
         mine += head_units(c, g) * a.n_kv_heads;
     }
     long long upto_b = mine;
@@ -314,17 +339,23 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     }
     if (threadIdx.x == 0) ws.desc[cta].valid = 0;
     fence_before_sync();
-    __syncthreads();
+    spare = __syncthreads_or(spare);
     fence_after_sync();
+    if (cta == 0 && threadIdx.x == 0) *ws.spare = spare;
     const uint32_t tmem = sh.tmem;
     const uint32_t full0 = smem_addr(&sh.full[0]), empty0 = smem_addr(&sh.empty[0]);
 
     if (warp >= kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int n_box = kTileKeys / box_keys;
-        // a piece's K or V tiles into their ring, from ring position `pos` on; around_first() runs ahead of and behind the first tile
-        auto load_tiles = [&](const Piece& p, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto around_first) {
+        // A piece's K or V tiles into their ring, from ring position `pos` on; around_first() runs ahead of and behind the first tile.
+        // A weight of zero must keep out what it stands for, but 0 * NaN is NaN.  So in V tiles with keys that some row does not
+        // see, slots at and behind the item's last key, which may hold anything, are cleared, and of the chunk's own tokens
+        // infinities and NaN: rows that see those get them back at the end.
+        int cleaned = 0;
+        auto load_tiles = [&](const Piece& p, const bool is_v, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto around_first) {
             const int kv_end = p.base + p.tok0 + p.n_tok, n = p.kv1 - p.kv0, box0 = p.kv0 * n_box;
+            const int item_sees = p.base + 1 + (a.c.parent ? 0 : p.tok0);  // every row of the item does, if it sees anything
             PageWindow w;
             PageWindow::fetch(a.c, p.b, box0, box_keys, kv_end, w.page, w.in);
             PageWindow::fetch(a.c, p.b, box0 + 32, box_keys, kv_end, w.page_next, w.in_next);
@@ -343,14 +374,48 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 const int keys = kv_end - (p.kv0 + i) * kTileKeys;  // of the item, from this tile on
                 const int boxes = keys >= kTileKeys ? n_box : (keys - 1) / box_keys + 1;
                 if (!warp_wait(empty + 8 * slot, (round & 1) ^ 1, gave_up)) return false;
-                if (lane == 0) mbar_expect(full + 8 * slot, (uint32_t)(boxes * box_keys * 128 * S::kHalves));
+                const bool clean = is_v && (p.kv0 + i + 1) * (int64_t)kTileKeys > item_sees;
+                const uint32_t bar = clean ? smem_addr(&sh.landed) : full + 8 * slot, tile = base + slot * S::kKvBytes;
+                if (lane == 0) mbar_expect(bar, (uint32_t)(boxes * box_keys * 128 * S::kHalves));
                 __syncwarp();
                 if (lane < boxes) {
-                    const uint32_t dst = base + slot * S::kKvBytes + lane * box_keys * 128;
+                    const uint32_t dst = tile + lane * box_keys * 128;
 #pragma unroll
-                    for (int hf = 0; hf < S::kHalves; ++hf) tma_load_4d(dst + hf * S::kKvHalf, map, full + 8 * slot, hf * 64, in, p.h, page);
+                    for (int hf = 0; hf < S::kHalves; ++hf) tma_load_4d(dst + hf * S::kKvHalf, map, bar, hf * 64, in, p.h, page);
                 }
                 __syncwarp();
+                if (clean) {
+                    if (!warp_wait(smem_addr(&sh.landed), cleaned & 1, gave_up)) return false;
+                    ++cleaned;
+                    const int end = min(kTileKeys, keys);
+                    // 16-byte pieces, 8 lanes a row
+                    for (int r = max(0, item_sees - (p.kv0 + i) * kTileKeys) + (lane >> 3); r < end; r += 4)
+#pragma unroll
+                        for (int hf = 0; hf < S::kHalves; ++hf) {
+                            const uint32_t piece = tile + hf * S::kKvHalf + r * 128 + (lane & 7) * 16;
+                            uint32_t x[4];
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(piece) : "memory");
+                            constexpr uint32_t kExp = std::is_same<E, __half>::value ? 0x7c00u : 0x7f80u;
+                            bool odd = false;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const bool lo = (x[k] & kExp) == kExp, hi = (x[k] & (kExp << 16)) == kExp << 16;
+                                odd = odd || lo || hi;
+                                x[k] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+                            }
+                            if (odd) {
+                                *static_cast<volatile int*>(&sh.not_finite) = 1;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                            }
+                        }
+                    for (int r = end + (lane >> 3); r < kTileKeys; r += 4)
+#pragma unroll
+                        for (int hf = 0; hf < S::kHalves; ++hf)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + hf * S::kKvHalf + r * 128 + (lane & 7) * 16), "r"(0) : "memory");
+                    fence_async_proxy();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full + 8 * slot);
+                }
                 if (i == 0 && !around_first(false)) return false;
                 if (++slot == slots) { slot = 0; ++round; }
             }
@@ -425,7 +490,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     }
                     return true;
                 };
-                ok = load_tiles(p, &map_k, ring, full0, empty0, S::kKSlots, pos, load_q);
+                ok = load_tiles(p, false, &map_k, ring, full0, empty0, S::kKSlots, pos, load_q);
                 if (!ok) break;
                 pos += p.kv1 - p.kv0;
             }
@@ -441,7 +506,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[ps]));
                 if (p.n_tok == 0) break;
-                ok = load_tiles(p, &map_v, ring + S::kKSlots * S::kKvBytes, full0 + 8 * S::kKSlots, empty0 + 8 * S::kKSlots, S::kVSlots, pos,
+                ok = load_tiles(p, true, &map_v, ring + S::kKSlots * S::kKvBytes, full0 + 8 * S::kKSlots, empty0 + 8 * S::kKSlots, S::kVSlots, pos,
                                 [](bool) { return true; });
                 if (!ok) break;
                 pos += p.kv1 - p.kv0;
@@ -534,7 +599,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor memory's lanes (bits 16 up)
         const uint32_t s_col = tmem + lanes + s * 128, o_col = tmem + lanes + 256 + s * 128;
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2);
-        int pos = 0, narrow_items = 0;
+        int narrow_items = 0;
         uint32_t done = 0, done_other = 0;  // steps of this stream and of the other one so far
         // the last of a stream's steps so far is in its sums.  Up to two products with V are pending, which one barrier's parity
         // could not tell apart.
@@ -566,6 +631,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 const bool reach = !valid || tree_line(a.c, p.b, tok, nodes, depth);
                 upto = reach ? p.base + 1 : 0;
             }
+            const int item_sees = p.base + 1 + (a.c.parent ? 0 : p.tok0);
             const int all_see = __reduce_min_sync(0xffffffffu, valid ? upto : 0x7fffffff);
             float m = -INFINITY, l = 0.0f;
             for (int st = s; ok && st < steps; st += 2) {
@@ -629,19 +695,6 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     l += sum.x + sum.y;
                     tmem_wait_st();
                 }
-                // slots at and behind the item's last key may hold anything: 0 * NaN must not reach the sums.  (Wide: both
-                // streams clear the tile, each ahead of its own product.)
-                if (key0 + kTileKeys > kv_end) {
-                    const int at = pos + j, slot = at % S::kVSlots;
-                    ok = ok && warp_wait(full0 + 8 * (S::kKSlots + slot), (at / S::kVSlots) & 1, gave_up);
-                    const uint32_t tile = ring + (S::kKSlots + slot) * S::kKvBytes + (row & 7) * 16;
-                    if (ok)
-                        for (int r = kv_end - key0 + (row >> 3); r < kTileKeys; r += 16)
-#pragma unroll
-                            for (int hf = 0; hf < S::kHalves; ++hf)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + hf * S::kKvHalf + r * 128), "r"(0) : "memory");
-                    fence_async_proxy();
-                }
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[s][buf]));
@@ -704,6 +757,10 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                         for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(v1[k]) * f1);
                     }
                     if (!valid) continue;
+                    if (!(l > 0.0f)) {  // nothing seen, whatever values that was
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = 0u;
+                    }
                     if (whole) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 8)
@@ -717,13 +774,17 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                             if (c + k < a.head_dim) *reinterpret_cast<uint4*>(po + c + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                     }
                 }
+                if (valid && *static_cast<volatile int*>(&sh.not_finite)) {
+                    const int lo = max(item_sees, p.kv0 * kTileKeys), hi = min(p.kv1 * kTileKeys, kv_end);
+                    restore_cleared<E>(a, p.b, p.h, lo, hi, upto, nodes, p.base + 1, c_lo, min(c_hi, a.head_dim), whole ? out : nullptr, po);
+                }
             }
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.o_free));
             if (threadIdx.x == 0 && has_first && !has_last)
                 ws.desc[cta] = SplitDesc{1, p.h, p.r0, p.tok0, p.n_tok, share_owner(shares, sh.open_unit), {0, 0}};
-            pos += n_tiles;
+
         }
     }
     fence_before_sync();
@@ -741,6 +802,7 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
     pdl_trigger();
     pdl_wait();
     constexpr int kPerLane = DP / 32;
+    const bool spare = n_cta == 0 || *ws.spare != 0;
     const int part = blockIdx.y * (kFinishThreads / 32) + warp, n_part = gridDim.y * (kFinishThreads / 32);
     if (blockIdx.x < (unsigned)n_cta) {
         const SplitDesc d = ws.desc[blockIdx.x];
@@ -780,7 +842,7 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
                     for (int k = 16; k; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
                     const float old = m;
                     m = fmaxf(m, mx);
-                    const float keep = old == -INFINITY ? 0.0f : exp2f(old - m), f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
+                    const float keep = m == old ? 1.0f : exp2f(old - m), f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
                     l *= keep;
 #pragma unroll
                     for (int k = 0; k < kPerLane; ++k) acc[k] *= keep;
@@ -812,13 +874,17 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
             }
         }
     }
-    // requests: status, rows that are no new token (with drafts shorter than their rows most of the batch), several warps a request
+    // Requests: status (last block row, which has the fewest rows to join), rows that are no new token (with drafts shorter than their
+    // rows most of the batch), several warps a request.
+    if (a.status && blockIdx.y == gridDim.y - 1)
+        for (int b = blockIdx.x * kFinishThreads + threadIdx.x; b < a.c.B; b += gridDim.x * kFinishThreads)
+            a.status[b] = load_chunk(a.c, b).bad ? HVD_REQ_BAD_LEN : HVD_REQ_OK;
+    if (!spare) return;
     const int n_warp = gridDim.x * gridDim.y * (kFinishThreads / 32), me = (blockIdx.y * gridDim.x + blockIdx.x) * (kFinishThreads / 32) + warp;
     const int share = max(1, n_warp / a.c.B), nvec = a.head_dim / 8;
-    for (int64_t x = me; x < (int64_t)a.c.B * share; x += n_warp) {
-        const int b = (int)(x % a.c.B), s = (int)(x / a.c.B);
+    for (uint32_t x = me; x < (uint32_t)(a.c.B * share); x += n_warp) {
+        const int s = (int)(x / (uint32_t)a.c.B), b = (int)x - s * a.c.B;
         const Chunk c = load_chunk(a.c, b);
-        if (a.status && s == 0 && lane == 0) a.status[b] = c.bad ? HVD_REQ_BAD_LEN : HVD_REQ_OK;
         for (int64_t i = (int64_t)c.n_new + s; i < c.rows; i += share) {
             const int64_t row = c.r0 + i;
             if (!HVD_IN_BOUNDS(a.c.dev_error, row, 0, a.c.total_rows)) continue;
@@ -872,6 +938,7 @@ hvd_status run(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream) {
     ws.o = reinterpret_cast<float*>(p);
     ws.ml = reinterpret_cast<float2*>(p + (size_t)n_cta * 2 * 256 * DP * sizeof(float));
     ws.desc = reinterpret_cast<SplitDesc*>(ws.ml + (size_t)n_cta * 2 * 256);
+    ws.spare = reinterpret_cast<int*>(ws.desc + n_cta);
     // query boxes: as few tokens as fill whole groups of 8 rows, so that every box starts on a 1024-byte boundary
     int box_tok = 8 / gcd(a.group, 8);
     if (box_tok * a.group > kTileRows) box_tok = kTileRows / a.group;
@@ -903,7 +970,7 @@ hvd_status run(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream) {
 
 size_t attn_workspace_bytes(int num_sms, int head_dim) {
     const int dp = head_dim > 64 ? 128 : 64;
-    return (size_t)num_sms * (2 * 256 * (dp * sizeof(float) + sizeof(float2)) + sizeof(SplitDesc));
+    return (size_t)num_sms * (2 * 256 * (dp * sizeof(float) + sizeof(float2)) + sizeof(SplitDesc)) + 16;
 }
 
 hvd_status attn_setup(hvd_ctx* ctx) {

@@ -146,6 +146,53 @@ def test_slots_behind_the_chunk_may_hold_anything():
         check(p)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("hq", [2, 32])
+def test_infinite_tokens_stay_with_the_rows_that_see_them(hq, tree, dtype):
+    """NaN and infinities in k or v of some of the chunk's tokens: rows that do not see them come out as if they were zeros; rows
+    that do get the infinity or NaN in its elements (v) or NaN throughout (k)."""
+    kw = dict(lens=[100, 60, 0, 700], rows=[20, 33, 40, 65], sel=[19, 32, 39, 64], hq=hq, hkv=2, d=80, page=16, dtype=dtype,
+              tree=True if tree else None, bad=0.1, seed=3)
+    clean, p = R.Problem(**kw), R.Problem(**kw)
+    bad_v = {(0, 3): [5, 70], (0, 19): [0], (1, 1): [79], (1, 20): [8, 9], (2, 0): [1], (3, 40): [33], (3, 64): [2]}
+    bad_k = {(0, 7), (3, 50)}
+    for n, ((b, i), cols) in enumerate(bad_v.items()):
+        p.vd[b][p.lens[b] + i, :, cols] = [float("inf"), float("nan"), -float("inf")][n % 3]
+        clean.vd[b][p.lens[b] + i, :, cols] = 0
+    for b, i in bad_k:
+        p.kd[b][p.lens[b] + i] = float("nan")
+        clean.kd[b][p.lens[b] + i] = 0
+    out, lse = run(p.fill())
+    want = R.attention(clean)
+    hit = torch.zeros(p.total, p.d, dtype=torch.bool, device="cuda")
+    lost = torch.zeros(p.total, dtype=torch.bool, device="cuda")
+    for b in range(p.B):
+        for i in range(p.rows[b]):
+            s = R.sees(p, b, i)
+            for (bb, j), cols in bad_v.items():
+                if bb == b and s[p.lens[b] + j]:
+                    hit[p.off[b] + i, cols] = True
+            lost[p.off[b] + i] = any(bb == b and s[p.lens[b] + j] for bb, j in bad_k)
+    assert hit.any() and lost.any() and not lost.all()
+    fine = ~hit & ~lost[:, None]
+    assert not torch.isfinite(out.float())[(hit & ~lost[:, None])[:, None].expand_as(out)].any()
+    mask = fine[:, None].expand_as(out)
+    got = torch.where(mask, out.float(), 0.0)
+    ls = torch.where(lost[:, None], 0.0, lse)
+    R.check_attention(clean, got, ls, (torch.where(mask, want[0], 0.0), torch.where(lost[:, None], 0.0, want[1]), *want[2:]))
+
+
+def test_values_of_the_prompt_that_are_infinite_leave_empty_rows_empty():
+    p = R.Problem(lens=[300, 40], rows=[9, 9], sel=[8, 8], hq=4, hkv=2, d=64, page=16, tree=True, seed=2)
+    p.parent[:, 4] = 60                                        # unreachable: sees nothing
+    for v in p.vd:
+        v[5] = float("nan")
+    out, lse = run(p.fill())
+    rows = [int(p.off[b]) + i for b in range(2) for i in range(9) if R.line_of(p.parent[b], i) is None]
+    assert (out[rows] == 0).all() and torch.isinf(lse[rows]).all() and len(rows) >= 2
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
