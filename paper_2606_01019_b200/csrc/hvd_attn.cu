@@ -37,6 +37,7 @@ constexpr int kThreads = 384;
 // registers: 384 threads start with 168 each; the softmax warpgroups take 208, the third keeps 88 (208 + 208 + 88 = 3 * 168)
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 constexpr int kFinishThreads = 256;
+constexpr int kJoin = 4;  // pieces whose sums are fetched together (6 and 8: 17 pieces of 4 rows 0.3 us faster, many items with few pieces 1 to 2 us slower)
 constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value (weights up to 2^8 are exact in either type)
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPieces = 4;             // pieces of work announced ahead
@@ -91,7 +92,7 @@ struct SplitDesc {
 
 struct Work {
     SplitDesc* desc;   // [CTAs]
-    float* o;          // [CTAs][2][256][DP]
+    float* o;          // [CTAs][2][DP / 4][256 rows][4]: a warp's rows side by side, for writing and for reading
     float2* ml;        // [CTAs][2][256] maximum (log2 units), sum
     int* spare;        // some row is no new token
 };
@@ -234,7 +235,7 @@ __device__ __noinline__ void restore_cleared(const AttnArgs& a, int b, int h, in
             const float e = (float)val[c];
             if (isfinite(e)) continue;
             if (out) out[c] = (E)((float)out[c] + e);
-            else part[c] += e;
+            else part[(c >> 2) * 1024 + (c & 3)] += e;
         }
     }
 }
@@ -740,7 +741,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     ws.ml[part_row] = make_float2(m, l);
                 }
                 E* const out = reinterpret_cast<E*>(a.out.p) + out_row * a.out.row_stride + (int64_t)head * a.out.head_stride;
-                float* const po = ws.o + part_row * DP;
+                float* const po = ws.o + (part_row & ~255ll) * DP + (part_row & 255) * 4;  // column c: + (c / 4) * 1024 + c % 4
                 const int c_lo = wide ? 0 : s * (DP / 2), c_hi = wide ? DP : c_lo + DP / 2;
                 const uint32_t o0 = tmem + lanes + 256 + (wide ? s * 128 : 0);
 #pragma unroll 1
@@ -771,7 +772,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     } else {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
-                            if (c + k < a.head_dim) *reinterpret_cast<uint4*>(po + c + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                            if (c + k < a.head_dim) *reinterpret_cast<uint4*>(po + (c + k) * 256) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                     }
                 }
                 if (valid && *static_cast<volatile int*>(&sh.not_finite)) {
@@ -794,93 +795,71 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
     if (threadIdx.x == 0 && sh.gave_up) atomicExch(a.c.dev_error, (int)HVD_DEV_WAIT_EXPIRED);
 }
 
-// Joins the pieces of the items that several CTAs shared (CTA x of the grid: the item that CTA x began and left
-// unfinished), and gives the rows that see nothing for want of a token their zeros.
+// Joins the pieces of the items that several CTAs shared (block x of the grid: the item that CTA x began and left
+// unfinished), and gives the rows that see nothing for want of a token their zeros.  A warp takes 32 rows by 8 columns.
 template <typename E, int DP>
 __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnArgs a, const Work ws, const int n_cta, const int tile_tok) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
     pdl_wait();
-    constexpr int kPerLane = DP / 32;
+    const int n_warp = gridDim.x * gridDim.y * (kFinishThreads / 32), me = (blockIdx.y * gridDim.x + blockIdx.x) * (kFinishThreads / 32) + warp;
     const bool spare = n_cta == 0 || *ws.spare != 0;
-    const int part = blockIdx.y * (kFinishThreads / 32) + warp, n_part = gridDim.y * (kFinishThreads / 32);
-    if (blockIdx.x < (unsigned)n_cta) {
-        const SplitDesc d = ws.desc[blockIdx.x];
-        if (d.valid) {
-            const int rows = d.n_tok * a.group, n = d.c_last - (int)blockIdx.x + 1;
-            for (int r = part; r < rows; r += n_part) {
-                // row r of the item: token r / group; its place among the partial sums
-                const int t = r / a.group, grp = r - t * a.group;
-                const int place = t < tile_tok ? r : 128 + r - tile_tok * a.group;
-                auto slot = [&](int i) { return (int64_t)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)) * 256 + place; };
-                const float* const o = ws.o + lane * kPerLane;
-                const bool mine = lane * kPerLane < a.head_dim;
-                float acc[kPerLane] = {}, l = 0.0f, m = -INFINITY;
-                float v[8][kPerLane];
-                auto fetch = [&](int i) {  // eight pieces' sums from piece i on
+    const int chunks = a.head_dim / 8, at = blockIdx.x;
+    SplitDesc d = {};
+    if (at < n_cta) d = ws.desc[at];
+    const int rows = d.valid ? d.n_tok * a.group : 0, n = d.c_last - at + 1;
+    for (int u = blockIdx.y * (kFinishThreads / 32) + warp; u < (rows + 31) / 32 * chunks; u += gridDim.y * (kFinishThreads / 32)) {
+        const int block = u / chunks, ch = u - block * chunks, row = block * 32 + lane;
+        if (row >= rows) continue;
+        // row of the item: token row / group; its place among the partial sums
+        const int t = row / a.group, grp = row - t * a.group;
+        const int place = t < tile_tok ? row : 128 + row - tile_tok * a.group;
+        float acc[8] = {}, l = 0.0f, m = -INFINITY;
+        for (int i0 = 0; i0 < n; i0 += kJoin) {  // rescaled to the largest maximum so far
+            float2 ml[kJoin];
+            float4 o[kJoin][2];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-#pragma unroll
-                        for (int k = 0; k < kPerLane; ++k) v[u][k] = 0.0f;
-                        if (i + u < n && mine) {
-                            const float* q = o + slot(i + u) * DP;
-                            if constexpr (kPerLane == 4) {
-                                const float4 w = *reinterpret_cast<const float4*>(q);
-                                v[u][0] = w.x; v[u][1] = w.y; v[u][2] = w.z; v[u][3] = w.w;
-                            } else {
-                                const float2 w = *reinterpret_cast<const float2*>(q);
-                                v[u][0] = w.x; v[u][1] = w.y;
-                            }
-                        }
-                    }
-                };
-                fetch(0);  // while the maxima come in
-                for (int i0 = 0; i0 < n; i0 += 32) {  // 32 pieces at a time, rescaled to the largest maximum so far
-                    const float2 ml = i0 + lane < n ? ws.ml[slot(i0 + lane)] : make_float2(-INFINITY, 0.0f);
-                    float mx = ml.x;
-#pragma unroll
-                    for (int k = 16; k; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
-                    const float old = m;
-                    m = fmaxf(m, mx);
-                    const float keep = m == old ? 1.0f : exp2f(old - m), f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
-                    l *= keep;
-#pragma unroll
-                    for (int k = 0; k < kPerLane; ++k) acc[k] *= keep;
-                    float li = ml.y * f;
-#pragma unroll
-                    for (int k = 16; k; k >>= 1) li += __shfl_xor_sync(0xffffffffu, li, k);
-                    l += li;
-                    const int e = min(32, n - i0);
-                    for (int i = 0; i < e; i += 8) {
-                        if (i0 + i > 0) fetch(i0 + i);
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const float fi = __shfl_sync(0xffffffffu, f, (i + u) & 31);
-#pragma unroll
-                            for (int k = 0; k < kPerLane; ++k) acc[k] += v[u][k] * fi;
-                        }
-                    }
+            for (int k = 0; k < kJoin; ++k) {
+                ml[k] = make_float2(-INFINITY, 0.0f);
+                o[k][0] = o[k][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (i0 + k < n) {
+                    const int64_t slot = 2 * (at + i0 + k) + (i0 + k == 0 ? 1 : 0);
+                    ml[k] = ws.ml[slot * 256 + place];
+                    const float* q = ws.o + (slot * (DP / 4) + 2 * ch) * 1024 + place * 4;
+                    o[k][0] = *reinterpret_cast<const float4*>(q);
+                    o[k][1] = *reinterpret_cast<const float4*>(q + 1024);
                 }
-                const int64_t row = d.r0 + d.tok0 + t;
-                const int head = d.h * a.group + grp;
-                if (!HVD_IN_BOUNDS(a.c.dev_error, row, 0, a.c.total_rows)) continue;
-                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                if (mine) {
-                    uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<E*>(a.out.p) + row * a.out.row_stride + (int64_t)head * a.out.head_stride + lane * kPerLane);
+            }
+            const float old = m;
 #pragma unroll
-                    for (int k = 0; k < kPerLane / 2; ++k) out[k] = pack2<E>(acc[2 * k] * inv, acc[2 * k + 1] * inv);
-                }
-                if (a.lse && lane == 0) a.lse[row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            for (int k = 0; k < kJoin; ++k) m = fmaxf(m, ml[k].x);
+            if (m == -INFINITY) continue;
+            const float keep = exp2_approx(old - m);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] *= keep;
+            l *= keep;
+#pragma unroll
+            for (int k = 0; k < kJoin; ++k) {
+                const float f = exp2_approx(ml[k].x - m);
+                l += ml[k].y * f;
+                acc[0] += o[k][0].x * f; acc[1] += o[k][0].y * f; acc[2] += o[k][0].z * f; acc[3] += o[k][0].w * f;
+                acc[4] += o[k][1].x * f; acc[5] += o[k][1].y * f; acc[6] += o[k][1].z * f; acc[7] += o[k][1].w * f;
             }
         }
+        const int64_t out_row = d.r0 + d.tok0 + t;
+        const int head = d.h * a.group + grp;
+        if (!HVD_IN_BOUNDS(a.c.dev_error, out_row, 0, a.c.total_rows)) continue;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        *reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.out.p) + out_row * a.out.row_stride + (int64_t)head * a.out.head_stride + 8 * ch) =
+            make_uint4(pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[2] * inv, acc[3] * inv), pack2<E>(acc[4] * inv, acc[5] * inv),
+                       pack2<E>(acc[6] * inv, acc[7] * inv));
+        if (a.lse && ch == 0) a.lse[out_row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
-    // Requests: status (last block row, which has the fewest rows to join), rows that are no new token (with drafts shorter than their
-    // rows most of the batch), several warps a request.
+    // Requests: status, rows that are no new token (with drafts shorter than their rows most of the batch), several warps a request.
     if (a.status && blockIdx.y == gridDim.y - 1)
         for (int b = blockIdx.x * kFinishThreads + threadIdx.x; b < a.c.B; b += gridDim.x * kFinishThreads)
             a.status[b] = load_chunk(a.c, b).bad ? HVD_REQ_BAD_LEN : HVD_REQ_OK;
     if (!spare) return;
-    const int n_warp = gridDim.x * gridDim.y * (kFinishThreads / 32), me = (blockIdx.y * gridDim.x + blockIdx.x) * (kFinishThreads / 32) + warp;
     const int share = max(1, n_warp / a.c.B), nvec = a.head_dim / 8;
     for (uint32_t x = me; x < (uint32_t)(a.c.B * share); x += n_warp) {
         const int s = (int)(x / (uint32_t)a.c.B), b = (int)x - s * a.c.B;
@@ -959,9 +938,9 @@ hvd_status run(hvd_ctx* ctx, const AttnArgs& a, bool f16, cudaStream_t stream) {
         e = launch_kernel(pdl, attn_tile_kernel<E, DP>, dim3(n_cta), dim3(kThreads), kSmemBytes<DP>, stream, a, ws, Geometry{tile_tok, 2 * tile_tok}, box_keys, box_tok, mq, mk, mv);
         if (e != cudaSuccess) return cuda_fail(ctx, e, "attn_tile_kernel");
     }
-    // a warp joins a row at a time: blocks for as many rows as an item can have here, four a warp
-    const int64_t most_rows = c.total_rows * a.group < 256 ? c.total_rows * a.group : 256;
-    const int by = (int)((most_rows + 31) / 32 > 1 ? (most_rows + 31) / 32 : 1);
+    // blocks for as many units as an item can have here, eight at most: the SMs hold so many at once
+    const int64_t units = ((c.total_rows * a.group < 256 ? c.total_rows * a.group : 256) + 31) / 32 * (a.head_dim / 8);
+    const int by = units > 56 ? 8 : units > 8 ? (int)((units + 7) / 8) : 1;
     e = launch_kernel(pdl, attn_finish_kernel<E, DP>, dim3(n_cta, by), dim3(kFinishThreads), 0, stream, a, ws, c.total_rows > 0 ? n_cta : 0, tile_tok);
     return e == cudaSuccess ? HVD_OK : cuda_fail(ctx, e, "attn_finish_kernel");
 }
