@@ -70,6 +70,12 @@ def test_rows_from_k_uniform_and_ragged_selection():
         assert (out[r] == 0).all() and torch.isinf(lse[r]).all()
 
 
+@pytest.mark.parametrize("B", [383, 384, 385, 900, 2100])
+def test_batches_of_more_requests_than_a_cta_has_threads(B):
+    rng = np.random.default_rng(B)
+    check(R.Problem(lens=[int(x) for x in rng.integers(0, 200, B)], rows=[int(x) for x in rng.integers(0, 4, B)], hq=6, hkv=3, d=32, page=16, seed=B))
+
+
 def test_many_rows_that_are_no_new_token():
     """Short drafts in wide blocks of rows, as a ragged batch has them: the other rows come out as zeros."""
     rng = np.random.default_rng(4)
