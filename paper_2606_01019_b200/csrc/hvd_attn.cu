@@ -23,7 +23,7 @@
 // Measured on one B200, calls in a row in a graph: 64 requests of 16 K tokens with 17 rows, 32/8 heads of 128: 681 us for 4.3 GB of keys
 // and values (6.3 TB/s, bound by HBM); 96 ragged requests, one row: 491 us (6.2 TB/s); 4 x 2047 rows behind 1.5 to 9 K tokens: 715 us
 // (971 TFLOP/s; bound by the alternation of products and softmax: 1860 cycles a pair of steps, the products alone 1285); one token
-// behind 1037: 13.9 us (two launches and their round trips).  Key tiles of 64 instead of 128: with 128 a stream's scores, weights and sums
+// behind 1037: 13.6 us (two launches and their round trips).  Key tiles of 64 instead of 128: with 128 a stream's scores, weights and sums
 // leave no room for a second buffer, and six tiles in flight hide HBM better than two and a half (one-token decode 104 -> 93 us).
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -44,6 +44,7 @@ constexpr int kThreads = 384;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 constexpr int kFinishThreads = 256;
 constexpr int kJoin = 4;  // pieces whose sums are fetched together (6 and 8: 17 pieces of 4 rows 0.3 us faster, many items with few pieces 1 to 2 us slower)
+constexpr int kShortPiece = 32;         // key tiles; below, only the query boxes that hold tokens are loaded
 constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value (either type holds weights of 2^8 as well as of 1)
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPieces = 4;             // pieces of work announced ahead
@@ -482,9 +483,11 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     if (!warp_wait(smem_addr(&sh.q_empty), (items & 1) ^ 1, gave_up)) return false;
                     // Boxes behind the item's tokens lie outside the tensor and bring zeros: rows of zeros make scores and weights of
                     // zero, which cost the tensor cores less power than what the shared memory held (ragged decode, in a long run,
-                    // 590 -> 549 us).
+                    // 590 -> 549 us).  A short piece goes without them, its unused rows hold what was there and nothing reads what
+                    // comes of them: power does not bound it, and issuing all boxes keeps its first keys waiting (one token 14.0 ->
+                    // 13.6 us, 4 x 2 K 21.4 -> 21.0 us; from 8 to 32 tiles the border makes no difference).
                     const int nb = g.tile_tok / box_tok;  // boxes of a row tile
-                    const int n_box_q = p.n_tok > g.tile_tok ? 2 * nb : nb;
+                    const int n_box_q = p.kv1 - p.kv0 < kShortPiece ? (p.n_tok + box_tok - 1) / box_tok : p.n_tok > g.tile_tok ? 2 * nb : nb;
                     if (lane == 0) mbar_expect(smem_addr(&sh.q_full), (uint32_t)(n_box_q * box_tok * a.group * 128 * S::kHalves));
                     __syncwarp();
                     for (int x = lane; x < n_box_q; x += 32) {

@@ -144,6 +144,25 @@ def test_maxima_that_climb_and_fall():
     check(p)
 
 
+@pytest.mark.parametrize("hq,d,dtype", [(1, 128, BF), (4, 128, BF), (16, 64, HF)])
+def test_queries_that_are_nan_stay_in_their_own_request(hq, d, dtype):
+    """Requests of one row are worked on where requests of whole row tiles were before them: what those left in the part of the
+    query tile that one row does not use reaches no result, not by one bit."""
+    rng = np.random.default_rng(hq)
+    B = 600
+    rows = [int(rng.integers(64, 300)) // hq + 1 if b % 2 == 0 else int(rng.integers(1, 4)) for b in range(B)]
+    p = R.Problem(lens=[int(x) for x in rng.integers(0, 400, B)], rows=rows, hq=hq, hkv=1, d=d, page=16, dtype=dtype, seed=hq).fill()
+    out, lse = run(p)
+    want = R.attention(p)
+    R.check_attention(p, out, lse, want)
+    short = np.concatenate([np.arange(p.off[b], p.off[b + 1]) for b in range(1, B, 2)])
+    wide = np.concatenate([np.arange(p.off[b], p.off[b + 1]) for b in range(0, B, 2)])
+    q = p.q.clone()
+    q[wide] = torch.tensor([float("nan"), float("inf"), 60000.0], dtype=dtype, device=q.device)[torch.arange(len(wide), device=q.device) % 3][:, None, None]
+    got, got_lse = run(p, q=q)
+    assert torch.equal(got[short], out[short]) and torch.equal(got_lse[short], lse[short])
+
+
 def test_slots_behind_the_chunk_may_hold_anything():
     for fill in (float("nan"), float("inf"), -float("inf"), 3.0e38):
         p = R.Problem(lens=[100, 37, 127, 0], rows=[3, 1, 1, 1], hq=4, hkv=2, d=128, page=64, seed=4)
