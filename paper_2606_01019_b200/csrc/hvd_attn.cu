@@ -228,6 +228,11 @@ __device__ __forceinline__ float2 weights(const uint32_t (&x)[2][32], uint32_t d
     return add2(sum[0], sum[1]);
 }
 
+// Row statistics (m, l) with l = 0: m = -infinity of a row that sees nothing, kLowest of one whose scores are all -infinity (0 / 0).
+constexpr float kLowest = -3.402823466e38f;
+__device__ __forceinline__ float inverse_sum(float m, float l) { return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : 1.0f / l; }
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
+
 // Infinities and NaN that were cleared from the values of tokens [lo, hi), back into a row that sees them: columns [c0, c1) of its
 // output, or of its partial sums.  (Any positive weight times such a value is that value.)
 template <typename E>
@@ -673,17 +678,19 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                         const uint32_t* v = &x[i >> 1][(i & 1) * 16];
                         top[i] = __uint_as_float(v[0]);
 #pragma unroll
-                        for (int k = 1; k < 15; k += 2) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
-                        top[i] = fmaxf(top[i], __uint_as_float(v[15]));
+                        for (int k = 1; k < 15; k += 2) top[i] = max_nan(top[i], __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                        top[i] = max_nan(top[i], __uint_as_float(v[15]));
                     }
-                    const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                    // A NaN among the scores makes the maximum NaN from here on, and with it weights and sum (but for the columns of
+                    // exp2_poly, which come out as some number).
+                    const float mt = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.scale_log2;
                     if (st < 2) {
                         m = mt;
                     } else {
-                        const bool grown = valid && mt > m + kRescaleAbove;
+                        const bool grown = valid && !(mt <= m + kRescaleAbove);  // or NaN
                         if (__any_sync(0xffffffffu, grown)) {
                             const float old = m;
-                            m = fmaxf(m, mt);
+                            m = max_nan(m, mt);
                             const float f = m == -INFINITY ? 1.0f : exp2_approx(old - m);
                             l *= f;
                             ok = sums_done(s, done);  // the step before
@@ -713,7 +720,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             if (!ok) break;
             done_other += s ? (steps + 1) / 2 : steps / 2;
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
-            if (m == -INFINITY) l = 0.0f;  // nothing seen: exp2_poly leaves 2^-126 each
+            if (m == -INFINITY) l = 0.0f;  // weights of zero: exp2_poly leaves 2^-126 each
             // every warp is through with the item before
             if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
             if (!wide) {  // maxima and sums of both streams
@@ -732,20 +739,21 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 float f0 = 1.0f, f1 = 0.0f;  // weights of the sums read below
                 if (!wide) {
                     const float m0 = sh.m[0][row], m1 = sh.m[1][row];
-                    m = fmaxf(m0, m1);
+                    m = max_nan(m0, m1);
                     f0 = m0 == -INFINITY ? 0.0f : exp2_approx(m0 - m);
                     f1 = m1 == -INFINITY ? 0.0f : exp2_approx(m1 - m);
-                    l = sh.l[0][row] * f0 + (f1 > 0.0f ? sh.l[1][row] * f1 : 0.0f);
+                    l = sh.l[0][row] * f0 + sh.l[1][row] * f1;
                 }
+                if (has_first && m == -INFINITY && upto > 0) m = kLowest;  // a row that sees anything sees key 0
                 const bool two = !wide && steps > 1;
                 const int64_t out_row = p.r0 + tok;
                 const int head = p.h * a.group + grp;
                 const int64_t part_row = (int64_t)(2 * cta + (has_first ? 1 : 0)) * 256 + (wide ? s * 128 : 0) + row;
                 if (whole) {
-                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                    const float inv = inverse_sum(m, l);
                     f0 *= inv;
                     f1 *= inv;
-                    if (valid && a.lse && (wide || s == 0)) a.lse[out_row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                    if (valid && a.lse && (wide || s == 0)) a.lse[out_row * a.n_q_heads + head] = log_sum(m, l);
                 } else if (valid && (wide || s == 0)) {
                     ws.ml[part_row] = make_float2(m, l);
                 }
@@ -767,7 +775,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                         for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(v1[k]) * f1);
                     }
                     if (!valid) continue;
-                    if (!(l > 0.0f)) {  // nothing seen, whatever values that was
+                    if (whole ? m == -INFINITY : l == 0.0f) {  // nothing seen, or nothing of this piece, whatever values that was
 #pragma unroll
                         for (int k = 0; k < 32; ++k) v[k] = 0u;
                     }
@@ -841,7 +849,7 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
             }
             const float old = m;
 #pragma unroll
-            for (int k = 0; k < kJoin; ++k) m = fmaxf(m, ml[k].x);
+            for (int k = 0; k < kJoin; ++k) m = max_nan(m, ml[k].x);
             if (m == -INFINITY) continue;
             const float keep = exp2_approx(old - m);
 #pragma unroll
@@ -858,11 +866,11 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const AttnA
         const int64_t out_row = d.r0 + d.tok0 + t;
         const int head = d.h * a.group + grp;
         if (!HVD_IN_BOUNDS(a.c.dev_error, out_row, 0, a.c.total_rows)) continue;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = inverse_sum(m, l);
         *reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.out.p) + out_row * a.out.row_stride + (int64_t)head * a.out.head_stride + 8 * ch) =
             make_uint4(pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[2] * inv, acc[3] * inv), pack2<E>(acc[4] * inv, acc[5] * inv),
                        pack2<E>(acc[6] * inv, acc[7] * inv));
-        if (a.lse && ch == 0) a.lse[out_row * a.n_q_heads + head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        if (a.lse && ch == 0) a.lse[out_row * a.n_q_heads + head] = log_sum(m, l);
     }
     // Requests: status, rows that are no new token (with drafts shorter than their rows most of the batch), several warps a request.
     if (a.status && blockIdx.y == gridDim.y - 1)

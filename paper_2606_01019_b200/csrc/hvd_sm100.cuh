@@ -161,6 +161,19 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
+// the largest; NaN if any is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
 // two 32-bit operations in one instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;

@@ -218,6 +218,89 @@ def test_values_of_the_prompt_that_are_infinite_leave_empty_rows_empty():
     assert (out[rows] == 0).all() and torch.isinf(lse[rows]).all() and len(rows) >= 2
 
 
+def check_but(lost, p, out, lse, want):
+    """The rows and heads of `lost` [total, hq] are NaN throughout, the others as in 64 bits."""
+    assert lost.any()
+    assert torch.isnan(out[lost]).all() and torch.isnan(lse[lost]).all()
+    keep = ~lost
+    rest = lambda x: torch.where(keep[..., None], x, 0.0)
+    R.check_attention(p, rest(out.float()), torch.where(keep, lse, 0.0),
+                      (rest(want[0]), torch.where(keep, want[1], 0.0), rest(want[2]), want[3]))
+
+
+def rows_that_see(p, b, t):
+    """[total] rows of the batch that see token t of request b."""
+    s = torch.zeros(p.total, dtype=torch.bool, device="cuda")
+    for i in range(p.rows[b]):
+        s[p.off[b] + i] = bool(R.sees(p, b, i)[t])
+    return s
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 2), (32, 1)])
+def test_a_nan_key_makes_the_rows_that_see_it_nan(hq, hkv, tree, dtype):
+    """Keys of the prompt and of the chunk, the only key of a row among them; items of one piece and of many."""
+    kw = dict(lens=[0, 100, 0, 9000, 60], rows=[1, 20, 33, 9, 30], sel=[0, 19, 32, 8, 29], hq=hq, hkv=hkv, d=64, page=16, dtype=dtype,
+              tree=True if tree else None, bad=0.1, seed=21)
+    clean, p = R.Problem(**kw), R.Problem(**kw)
+    lost = torch.zeros(p.total, dtype=torch.bool, device="cuda")
+    for b, t in ((0, 0), (1, 100 + 5), (1, 100 + 9), (2, 3), (3, 4003), (4, 60 + 8)):
+        p.kd[b][t] = float("nan")
+        clean.kd[b][t] = 0
+        lost |= rows_that_see(p, b, t)
+    assert not lost.all()
+    out, lse = run(p.fill())
+    check_but(lost[:, None].expand(p.total, hq), p, out, lse, R.attention(clean))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("hq,hkv,rows", [(1, 1, 1), (8, 2, 9), (8, 2, 40), (32, 1, 9)])
+def test_a_nan_query_makes_its_own_row_nan(hq, hkv, rows, dtype):
+    kw = dict(lens=[0, 37, 700, 20000], rows=[rows] * 4, hq=hq, hkv=hkv, d=64, page=16, dtype=dtype, seed=22)
+    clean, p = R.Problem(**kw), R.Problem(**kw)
+    lost = torch.rand(p.total, hq, generator=torch.Generator("cuda").manual_seed(1), device="cuda") < 0.3
+    lost[0, 0], lost[-1, -1] = True, True
+    p.q[lost] = float("nan")
+    clean.q[lost] = 0
+    out, lse = run(p.fill())
+    check_but(lost, p, out, lse, R.attention(clean))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,rows", [(0, 1), (30, 5), (200, 70), (9000, 3)])
+def test_scores_that_are_all_minus_infinity(n, rows, dtype):
+    """A row whose scores are all -infinity sees keys all the same: by the formula 0 / 0 in out, log 0 in lse.  Unreachable rows beside it
+    see nothing and come out as zeros."""
+    nodes = rows - 1
+    p = R.Problem(lens=[n, 50], rows=[rows, rows], sel=[min(nodes, 64), nodes], hq=4, hkv=1, d=64, page=16, dtype=dtype, tree=True, bad=0.3, seed=23)
+    q, k = p.q, p.kd[0]
+    q[..., 0] = 1.0
+    k[:, :, 0] = -float("inf")
+    out, lse = run(p.fill())
+    seen = torch.tensor([bool(R.sees(p, 0, i).any()) for i in range(rows)], device="cuda")
+    first, first_lse = out[:rows], lse[:rows]
+    assert torch.isnan(first[seen]).all() and (first[~seen] == 0).all()
+    assert (first_lse == -float("inf")).all()
+    want = R.attention(p)
+    there = torch.arange(p.total, device="cuda")[:, None] >= rows
+    mass = float(torch.einsum("rhd,nd->hrn", q[rows:].double().abs(), p.kd[1][:, 0].double().abs()).max()) / 8.0
+    R.check_attention(p, torch.where(there[..., None], out.float(), 0.0), torch.where(there, lse, 0.0),
+                      (torch.where(there[..., None], want[0], 0.0), torch.where(there, want[1], 0.0), torch.where(there[..., None], want[2], 0.0), mass))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,hq", [(1, 4), (40, 8)])
+@pytest.mark.parametrize("n", [200, 5000])
+def test_a_nan_key_shows_at_every_column(n, rows, hq, dtype):
+    """Request c has its NaN key in column c of a tile."""
+    p = R.Problem(lens=[n] * 64, rows=[rows] * 64, hq=hq, hkv=1, d=64, page=16, dtype=dtype, seed=24)
+    for c in range(64):
+        p.kd[c][64 + c] = float("nan")
+    out, lse = run(p.fill())
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
