@@ -675,7 +675,7 @@ HVD_API hvd_status hvd_rope_append(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* 
  * type for the product with v.  Rows that see nothing (rows beyond n_new, unreachable nodes, skipped
  * requests) get out = 0 and lse = -inf; rows of no request are not written.  Slots at and behind cache_len + n_new may hold
  * anything, also NaN, and so may tokens of the chunk for the rows that do not see them.
- * A row that sees a score of NaN gets NaN in out and lse; one whose scores are all -infinity NaN in out (0 / 0) and lse = -inf.
+ * A row that sees a score of NaN or +infinity gets NaN in out and lse; one whose scores are all -infinity NaN in out (0 / 0) and lse = -inf.
  * A page entry outside [0, n_pages) stands for a page of zeros.
  *
  * q    HOST struct, [total_rows] rows of n_q_heads heads

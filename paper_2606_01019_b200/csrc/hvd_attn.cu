@@ -720,7 +720,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             if (!ok) break;
             done_other += s ? (steps + 1) / 2 : steps / 2;
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
-            if (m == -INFINITY) l = 0.0f;  // weights of zero: exp2_poly leaves 2^-126 each
+            // exp2_poly leaves 2^-126 where a weight is zero, and where a score of +infinity stands against itself
+            if (m == -INFINITY) l = 0.0f;
+            else if (m == INFINITY) l = NAN;
             // every warp is through with the item before
             if (items > 0) ok = warp_wait(smem_addr(&sh.o_free), (items & 1) ^ 1, gave_up);
             if (!wide) {  // maxima and sums of both streams

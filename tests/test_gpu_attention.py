@@ -301,6 +301,24 @@ def test_a_nan_key_shows_at_every_column(n, rows, hq, dtype):
     assert torch.isnan(out).all() and torch.isnan(lse).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,hq", [(1, 4), (40, 8)])
+@pytest.mark.parametrize("n", [200, 5000])
+def test_an_infinite_score_shows_at_every_column(n, rows, hq, dtype):
+    """Request c has its infinite key in column c of a tile.  Heads with a positive element make a score of +infinity of it (inf / inf
+    in out), the others one of -infinity: a weight of zero, like that of a score far below the rest."""
+    kw = dict(lens=[n] * 64, rows=[rows] * 64, hq=hq, hkv=1, d=64, page=16, dtype=dtype, seed=24)
+    clean, p = R.Problem(**kw), R.Problem(**kw)
+    up = torch.arange(hq, device="cuda") % 2 == 0
+    p.q[..., 0] = torch.where(up, 1.0, -1.0).to(dtype)
+    clean.q[..., 0] = p.q[..., 0]
+    for c in range(64):
+        p.kd[c][64 + c], clean.kd[c][64 + c] = 0.0, 0.0
+        p.kd[c][64 + c, :, 0], clean.kd[c][64 + c, :, 0] = float("inf"), 2000.0   # 250 below
+    out, lse = run(p.fill())
+    check_but(up[None].expand(p.total, hq), p, out, lse, R.attention(clean))
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
