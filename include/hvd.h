@@ -585,6 +585,7 @@ HVD_API const char* hvd_noalloc_last_error(void);
  * are 16-byte aligned, strides multiples of 8 elements, so that TMA can fetch the pages.
  * A request with cache_len < 0, cache_len + n_new > table_stride * page_size, rows outside
  * [0, total_rows) or (sel_len given) no row is skipped: status HVD_REQ_BAD_LEN.
+ * Offsets may run backwards or leave the rows: that spoils the requests that they bound, no others.  They must not give a row to two.
  * ---------------------------------------------------------------------------------------------------
  */
 

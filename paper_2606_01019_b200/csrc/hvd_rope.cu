@@ -48,7 +48,7 @@ struct Token {
     int b;        // -1: not a new token
 };
 
-// The request of a row: the last one whose rows start at or before it.  All threads of the CTA count starts.
+// The request of a row where the offsets ascend: the last one whose rows start at or before it.  All threads of the CTA count starts.
 __device__ __forceinline__ int request_of(const ChunkArgs& c, int64_t row) {
     if (!c.row_off) return (int)min(row / (c.k_uniform + 1), (int64_t)c.B);
     int lo = 0, hi = c.B;  // row_off[lo] <= row < row_off[hi], as far as the offsets ascend
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
     __shared__ Token tok[T];
     __shared__ __align__(16) float2 cs[T][HVD_MAX_HEAD_DIM / 2];
     __shared__ unsigned long long turns[HVD_MAX_HEAD_DIM / 2];
-    __shared__ int pos[T];
+    __shared__ int pos[T], owner[T];
     const ChunkArgs& c = a.c;
     pdl_trigger();
     pdl_wait();
@@ -174,29 +174,49 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
 
     for (int j = threadIdx.x; j < half; j += blockDim.x) turns[j] = a.turns[j];
     const int b0 = request_of(c, first);
-    if ((int)threadIdx.x < n_tok) {
-        const int i = threadIdx.x;
-        Token t = {first + i, -1, -1};
-        int b = b0;
-        if (c.row_off) while (b + 1 < c.B && c.row_off[b + 1] <= t.row) ++b;
-        else b = (int)min(t.row / (c.k_uniform + 1), (int64_t)c.B);
-        if (b < c.B) {
-            const Chunk ch = load_chunk(c, b);
-            const int64_t at = t.row - ch.r0;
-            if (!ch.bad && at >= 0 && at < ch.n_new) {
-                t.b = b;
-                const int p = ch.base + (int)at;
-                const int64_t page = page_of(c, b, p);
-                int depth = (int)at;
-                unsigned long long nodes;
-                if (c.parent) tree_line(c, b, (int)at, nodes, depth);
-                pos[i] = ch.base + depth;
-                if (page >= 0 && HVD_IN_BOUNDS(c.dev_error, t.row, 0, c.total_rows)) t.kv = slot_offset(c, page, p);
-            }
-        }
-        tok[i] = t;
+    const int64_t row = first + (int)threadIdx.x;  // this thread's token, the first n_tok threads
+    int b = b0;
+    if (c.row_off) {
+        if ((int)threadIdx.x < n_tok) while (b + 1 < c.B && c.row_off[b + 1] <= row) ++b;
+    } else {
+        b = (int)min(row / (c.k_uniform + 1), (int64_t)c.B);
     }
-    __syncthreads();
+    for (bool again = false;; again = true) {
+        bool astray = false;
+        if ((int)threadIdx.x < n_tok) {
+            const int i = threadIdx.x;
+            Token t = {row, -1, -1};
+            astray = true;
+            if (b < c.B) {
+                const Chunk ch = load_chunk(c, b);
+                const int64_t at = row - ch.r0;
+                astray = at < 0 || at >= ch.rows;
+                if (!ch.bad && at >= 0 && at < ch.n_new) {
+                    t.b = b;
+                    const int p = ch.base + (int)at;
+                    const int64_t page = page_of(c, b, p);
+                    int depth = (int)at;
+                    unsigned long long nodes;
+                    if (c.parent) tree_line(c, b, (int)at, nodes, depth);
+                    pos[i] = ch.base + depth;
+                    if (page >= 0 && HVD_IN_BOUNDS(c.dev_error, t.row, 0, c.total_rows)) t.kv = slot_offset(c, page, p);
+                }
+            }
+            tok[i] = t;
+        }
+        if (!__syncthreads_or(astray && c.row_off && !again)) break;
+        // Offsets that do not ascend led past a token's request: every request is asked, the first that has the row takes it.
+        if ((int)threadIdx.x < T) owner[threadIdx.x] = c.B;
+        __syncthreads();
+        for (int i = threadIdx.x; i < c.B; i += blockDim.x) {
+            const int64_t r0 = c.row_off[i], r1 = c.row_off[i + 1];
+            if (r0 >= 0 && r1 <= c.total_rows)
+                for (int t = 0; t < n_tok; ++t)
+                    if (first + t >= r0 && first + t < r1) atomicMin(&owner[t], i);
+        }
+        __syncthreads();
+        b = owner[min((int)threadIdx.x, T - 1)];
+    }
     for (int i = threadIdx.x; i < n_tok * half; i += blockDim.x) {
         const int t = i / half, j = i - t * half;
         if (tok[t].b >= 0) {

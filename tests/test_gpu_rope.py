@@ -137,6 +137,40 @@ def test_unusable_requests_and_pages():
     ctx.close()
 
 
+@pytest.mark.parametrize("off,total", [([0, 4, -7, 15, 20], 20), ([0, 100, 200, 4, 8, 12], 12), ([30, -1, 0, 5, 9], 9), ([0, 3, 3, 99, 9, 20], 20), (600, None),
+                                       (2000, None)])
+def test_requests_beside_bad_offsets_are_appended(off, total):
+    """Offsets that run backwards or leave the rows spoil the requests that they bound and no others."""
+    rng = np.random.default_rng(9)
+    if total is None:
+        rows = rng.integers(0, 4, off)
+        off = np.concatenate([[0], np.cumsum(rows)])
+        total = int(off[-1])
+        off[rng.choice(len(off) - 2, 40, replace=False) + 1] = rng.choice([-5, total + 1, 1 << 40, -(1 << 40)], 40)
+    off = np.asarray(off, np.int64)
+    B = len(off) - 1
+    p = R.Problem(lens=[int(x) for x in rng.integers(0, 40, B)], rows=[24] * B, hq=2, hkv=1, d=64, page=16, seed=B).device()
+    p.k.zero_(), p.v.zero_()
+    ctx = p.context()
+    x = torch.rand(total, 4, 64, device="cuda").to(BF) + 1
+    q, k, v = x.split([2, 1, 1], dim=1)
+    q_out = torch.full((total, 2, 64), 9.0, dtype=BF, device="cuda")
+    t_off = torch.as_tensor(off, device="cuda")
+    ctx.hvd_rope_append(B, p.cache(), p.t_len, t_off, 0, total, None, None, q, k, v, q_out, p.status)
+    good = (off[:-1] >= 0) & (off[1:] <= total) & (off[1:] >= off[:-1])
+    assert p.status.tolist() == [0 if g else 2 for g in good] and 0 < good.sum() < B
+    want, written = torch.zeros_like(p.v), np.zeros(total, bool)
+    for b in np.nonzero(good)[0]:
+        written[off[b]:off[b + 1]] = True
+        at = p.places(b, p.lens[b], p.lens[b] + int(off[b + 1] - off[b]))
+        want[at] = v[off[b]:off[b + 1]]
+    assert torch.equal(want, p.v)
+    up = torch.as_tensor(written, device="cuda")
+    assert (q_out[~up] == 9).all() and (q_out[up] != 9).any(2).all()
+    assert ctx.hvd_device_status() == 0
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits():
     p = R.Problem(lens=[500], rows=[5], hq=4, hkv=2, d=128, page=64, seed=14, pool_pages=(1 << 31) // (64 * 256) + 64)
     p.table[0, :8] = p.n_pages - 1 - np.arange(8)
