@@ -48,6 +48,9 @@ constexpr int kShortPiece = 32;         // key tiles; below, only the query boxe
 constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value (either type holds weights of 2^8 as well as of 1)
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPieces = 4;             // pieces of work announced ahead
+// Flags of items, of which the loading warp is at most kPieces ahead of a softmax warp: that one's flag is its own until it is through.
+constexpr int kFlags = 8;
+static_assert(kFlags > kPieces, "see above");
 
 template <int DP> struct Shape {
     static constexpr int kHalves = DP / 64;                         // 128-byte columns of a tile row
@@ -79,9 +82,9 @@ struct Shared {  // behind the tiles
     uint64_t landed;                             // a V tile that is cleaned before it is full
     uint64_t drain;
     Piece piece[kPieces];
+    int not_finite[kFlags];  // [item % kFlags] some value of the chunk's own tokens was infinite or NaN
     uint32_t tmem;
     int gave_up;
-    int not_finite;       // some value of a chunk's own tokens was infinite or NaN
     struct { int b, h, qt, kv, r0, n_new, base; } start;  // where the CTA's share begins
     long long start_left;
     long long open_unit;  // of the item that the share leaves unfinished: its last tile's first unit
@@ -279,7 +282,6 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             mbar_init(smem_addr(&sh.landed), 1);
             mbar_init(smem_addr(&sh.drain), 2);
             sh.gave_up = 0;
-            sh.not_finite = 0;
         }
         mbar_init_fence();
     }
@@ -366,6 +368,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
         // see, slots at and behind the item's last key, which may hold anything, are cleared, and of the chunk's own tokens
         // infinities and NaN: rows that see those get them back at the end.
         int cleaned = 0;
+        volatile int* not_finite = nullptr;  // the item's flag, in the warp that loads values
         auto load_tiles = [&](const Piece& p, const bool is_v, const CUtensorMap* map, uint32_t base, uint32_t full, uint32_t empty, int slots, int pos, auto around_first) {
             const int kv_end = p.base + p.tok0 + p.n_tok, n = p.kv1 - p.kv0, box0 = p.kv0 * n_box;
             const int item_sees = p.base + 1 + (a.c.parent ? 0 : p.tok0);  // every row of the item does, if it sees anything
@@ -417,7 +420,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                                 x[k] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
                             }
                             if (odd) {
-                                *static_cast<volatile int*>(&sh.not_finite) = 1;
+                                *not_finite = 1;
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
                             }
                         }
@@ -521,6 +524,9 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[ps]));
                 if (p.n_tok == 0) break;
+                not_finite = &sh.not_finite[items % kFlags];
+                if (lane == 0) *not_finite = 0;
+                __syncwarp();
                 ok = load_tiles(p, true, &map_v, ring + S::kKSlots * S::kKvBytes, full0 + 8 * S::kKSlots, empty0 + 8 * S::kKSlots, S::kVSlots, pos,
                                 [](bool) { return true; });
                 if (!ok) break;
@@ -794,7 +800,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                             if (c + k < a.head_dim) *reinterpret_cast<uint4*>(po + (c + k) * 256) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                     }
                 }
-                if (valid && *static_cast<volatile int*>(&sh.not_finite)) {
+                if (valid && *static_cast<volatile int*>(&sh.not_finite[items % kFlags])) {
                     const int lo = max(item_sees, p.kv0 * kTileKeys), hi = min(p.kv1 * kTileKeys, kv_end);
                     restore_cleared<E>(a, p.b, p.h, lo, hi, upto, nodes, p.base + 1, c_lo, min(c_hi, a.head_dim), whole ? out : nullptr, po);
                 }

@@ -319,6 +319,33 @@ def test_an_infinite_score_shows_at_every_column(n, rows, hq, dtype):
     check_but(up[None].expand(p.total, hq), p, out, lse, R.attention(clean))
 
 
+def test_a_non_finite_value_costs_its_own_item_only():
+    """2048 requests of one wide item each, some 14 to an SM.  One value of one chunk is NaN: whether that item is the first or the last
+    of its SM's makes no difference to the call's time (its own rows pay, 13 others do not: a factor of 14 otherwise, so 4 tells them apart)."""
+    B, rows = 2048, 64
+    p = R.Problem(lens=[64] * B, rows=[rows] * B, hq=4, hkv=1, d=64, page=64, seed=25).fill().device()
+    ctx, cache, out = p.context(), p.cache(), torch.empty_like(p.q)
+
+    def took(b):
+        at = p.places(b, 64 + rows - 1, 64 + rows)
+        was = p.v[at].clone()
+        p.v[at] = torch.where(torch.arange(64, device="cuda") == 5, float("nan"), was.float()).to(BF)
+        times = []
+        for _ in range(6):
+            s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            s.record()
+            ctx.hvd_attn_paged(B, cache, p.t_len, p.t_off, 0, p.total, None, None, p.q, out)
+            e.record()
+            e.synchronize()
+            times.append(s.elapsed_time(e))
+        assert torch.isnan(out[b * rows + rows - 1, :, 5]).all() and torch.isfinite(out[b * rows + rows - 2]).all()
+        p.v[at] = was
+        return min(times[2:])
+    first, last = took(0), took(B - 1)
+    assert first < 4 * last, (first, last)
+    ctx.close()
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
