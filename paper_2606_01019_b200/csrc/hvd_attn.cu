@@ -654,7 +654,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             }
             const int item_sees = p.base + 1 + (a.c.parent ? 0 : p.tok0);
             const int all_see = __reduce_min_sync(0xffffffffu, valid ? upto : 0x7fffffff);
-            float m = -INFINITY, l = 0.0f;
+            float m = -INFINITY, l = 0.0f, l_far = 0.0f;  // l: the sum of up to 32 steps, l_far: of those before
             for (int st = s; ok && st < steps; st += 2) {
                 const int j = wide ? st >> 1 : st, key0 = (p.kv0 + j) * kTileKeys;
                 const uint32_t buf = done & 1;
@@ -690,15 +690,21 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     // A NaN among the scores makes the maximum NaN from here on, and with it weights and sum (but for the columns of
                     // exp2_poly, which come out as some number).
                     const float mt = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.scale_log2;
-                    if (st < 2) {
-                        m = mt;
-                    } else {
+                    bool first = false;
+                    if ((st & 62) == 0) {  // a tile behind thousands, or behind one large weight, is small against the whole sum
+                        l_far += l;
+                        l = 0.0f;
+                        first = st < 2;
+                        if (first) m = mt;
+                    }
+                    if (!first) {
                         const bool grown = valid && !(mt <= m + kRescaleAbove);  // or NaN
                         if (__any_sync(0xffffffffu, grown)) {
                             const float old = m;
                             m = max_nan(m, mt);
                             const float f = m == -INFINITY ? 1.0f : exp2_approx(old - m);
                             l *= f;
+                            l_far *= f;
                             ok = sums_done(s, done);  // the step before
                             fence_after_sync();
                             if (ok) {
@@ -726,6 +732,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
             if (!ok) break;
             done_other += s ? (steps + 1) / 2 : steps / 2;
             const bool has_first = p.kv0 == 0, has_last = p.kv1 == p.nkv, whole = has_first && has_last;
+            l += l_far;
             // exp2_poly leaves 2^-126 where a weight is zero, and where a score of +infinity stands against itself
             if (m == -INFINITY) l = 0.0f;
             else if (m == INFINITY) l = NAN;

@@ -346,6 +346,30 @@ def test_a_non_finite_value_costs_its_own_item_only():
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n", [32767, 131071])
+def test_the_sum_of_many_small_weights(n, dtype):
+    """One key stands 17.5 above all the others, which together add n e^-17.5 to the sum of weights: to 32 bits a tile of them is a few units
+    in the last place of the whole.  Rounding of the sum below 2^-18 of it, of exponent and logarithm below 2^-22 of 20; 160 requests
+    of two heads on the same pages, so that most are worked on in one piece."""
+    import paper_2606_01019_b200 as H
+    B, page = 160, 64
+    pages = -(-(n + 1) // page)
+    k = torch.zeros(pages, page, 2, 64, dtype=dtype, device="cuda")
+    k[0, 0, :, 0] = 14.0
+    q = torch.zeros(B, 2, 64, dtype=dtype, device="cuda")
+    q[..., 0] = 10.0
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(B, pages).contiguous()
+    ctx = H.Context(max_batch=B, k_cap=1, max_hist_len=16, max_rows=B, max_vocab=8)
+    ctx.hvd_set_attention(n_q_heads=2, n_kv_heads=2, head_dim=64, dtype=H.BF16 if dtype is BF else H.F16)
+    out, lse = torch.empty_like(q), torch.empty(B, 2, device="cuda")
+    ctx.hvd_attn_paged(B, H.KvCache(k, k.clone(), table), torch.full((B,), n, dtype=torch.int32, device="cuda"), None, 0, B, None, None, q, out, lse)
+    e = (lse.double() - (17.5 + np.log1p(n * np.exp(-17.5)))).abs()
+    assert bool((e <= 2.0 ** -17 + 2.0 ** -22 * 20).all()), float(e.max())
+    assert ctx.hvd_device_status() == 0
+    ctx.close()
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
