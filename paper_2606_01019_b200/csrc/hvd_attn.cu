@@ -29,6 +29,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "hvd_attn.cuh"
 #include "hvd_sm100.cuh"
 
@@ -45,7 +47,11 @@ constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 constexpr int kFinishThreads = 256;
 constexpr int kJoin = 4;  // pieces whose sums are fetched together (6 and 8: 17 pieces of 4 rows 0.3 us faster, many items with few pieces 1 to 2 us slower)
 constexpr int kShortPiece = 32;         // key tiles; below, only the query boxes that hold tokens are loaded
-constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value (either type holds weights of 2^8 as well as of 1)
+constexpr float kRescaleAbove = 8.0f;  // log2: a maximum that grew by less keeps its old value
+// log2 of the weight of a row's maximum: 1, or 2^7 for f16, whose numbers end at 2^-24 below and 2^16 above.  A long context behind one
+// large weight adds up from small ones, which would be rounded to zero from 2^-25 on (131071 keys of 2^-25.2 each: 0.33 % of the
+// output); the sum has them all.  With kRescaleAbove weights reach 2^15.
+template <typename E> constexpr float kTopWeight = std::is_same<E, __half>::value ? 7.0f : 0.0f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPieces = 4;             // pieces of work announced ahead
 // Flags of items, of which the loading warp is at most kPieces ahead of a softmax warp: that one's flag is its own until it is through.
@@ -200,7 +206,7 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
     return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
-// w = exp2(x * scale - m) of a row's 64 scores, rounded to the cache's type and packed, into tensor memory over the scores; returns
+// w = exp2(x * scale - m) (m: the maximum less kTopWeight) of a row's 64 scores, rounded to the cache's type and packed, into tensor memory over the scores; returns
 // their sums before rounding.  Every eighth pair goes through exp2_poly, which relieves the special function unit but takes more power,
 // by which long runs are bound (2047 rows behind 1.5 to 9 K tokens, long runs, us: none 823, every 8th pair 791, 5th 811, 3rd 837,
 // 2nd 862; short runs are fastest with every 3rd).  That makes 2^-126 of a score of -infinity: where there are some (`edge`) those
@@ -689,7 +695,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     }
                     // A NaN among the scores makes the maximum NaN from here on, and with it weights and sum (but for the columns of
                     // exp2_poly, which come out as some number).
-                    const float mt = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.scale_log2;
+                    const float mt = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.scale_log2 - kTopWeight<E>;
                     bool first = false;
                     if ((st & 62) == 0) {  // a tile behind thousands, or behind one large weight, is small against the whole sum
                         l_far += l;

@@ -370,6 +370,36 @@ def test_the_sum_of_many_small_weights(n, dtype):
     ctx.close()
 
 
+@pytest.mark.parametrize("n", [2000, 32767, 131071])
+@pytest.mark.parametrize("rows", [1, 9])
+def test_many_small_weights_behind_a_large_one_f16(n, rows):
+    """One key stands 17.5 above all the others, whose values are 1 where its own is 0.  A weight that small is below half of f16's smallest
+    number; held against a maximum of 2^7 it is not lost.  Each is off by 2^-25 of 2^-7 at most, the result is rounded once; 320 requests
+    on the same pages, so that most are worked on in one piece."""
+    import paper_2606_01019_b200 as H
+    B, page, end = 320, 64, n + rows
+    pages = -(-end // page)
+    k, v = torch.zeros(pages, page, 1, 64, dtype=HF, device="cuda"), torch.ones(pages, page, 1, 64, dtype=HF, device="cuda")
+    k[0, 0, 0, 0], v[0, 0] = 14.0, 0.0
+    q = torch.zeros(B * rows, 16, 64, dtype=HF, device="cuda")
+    q[..., 0] = 10.0
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(B, pages).contiguous()
+    ctx = H.Context(max_batch=B, k_cap=16, max_hist_len=16, max_rows=B * rows, max_vocab=8)
+    ctx.hvd_set_attention(n_q_heads=16, n_kv_heads=1, head_dim=64, dtype=H.F16)
+    out, lse = torch.empty_like(q), torch.empty(B * rows, 16, device="cuda")
+    ctx.hvd_attn_paged(B, H.KvCache(k, v, table), torch.full((B,), n, dtype=torch.int32, device="cuda"), None, rows - 1, B * rows, None, None, q, out, lse)
+    seen = n + 1 + np.arange(rows)                       # keys of each row
+    tail = (seen - 1) * np.exp(-17.5)
+    want = torch.as_tensor(np.tile(tail / (1 + tail), B), device="cuda")[:, None, None]
+    tol = (2 * R.UNIT[HF] + 2.0 ** -18) * want + n * 2.0 ** -32 + 2.0 ** -25
+    e = (out.double() - want).abs()
+    assert bool((e <= tol).all()), float((e / tol).max())
+    want_lse = torch.as_tensor(np.tile(17.5 + np.log1p(tail), B), device="cuda")[:, None]
+    assert bool(((lse.double() - want_lse).abs() <= 2.0 ** -17 + 2.0 ** -22 * 20).all())
+    assert ctx.hvd_device_status() == 0
+    ctx.close()
+
+
 def test_unusable_requests_are_skipped():
     p = R.Problem(lens=[20, 20, 20, 20, 20], rows=[4, 5, 6, 3, 2], sel=[3, 4, 5, 2, 1], hq=4, hkv=2, d=64, page=16, seed=6).fill()
     want = R.attention(p)
