@@ -659,7 +659,8 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                 upto = reach ? p.base + 1 : 0;
             }
             const int item_sees = p.base + 1 + (a.c.parent ? 0 : p.tok0);
-            const int all_see = __reduce_min_sync(0xffffffffu, valid ? upto : 0x7fffffff);
+            // every row of the warp sees the whole of a tile that starts here or before (the first key behind a tile may be 2^31)
+            const int whole_to = __reduce_min_sync(0xffffffffu, valid ? upto : 0x7fffffff) - kTileKeys;
             float m = -INFINITY, l = 0.0f, l_far = 0.0f;  // l: the sum of up to 32 steps, l_far: of those before
             for (int st = s; ok && st < steps; st += 2) {
                 const int j = wide ? st >> 1 : st, key0 = (p.kv0 + j) * kTileKeys;
@@ -673,7 +674,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     tmem_ld32(x[1], s_col + buf * 64 + 32);
                     tmem_wait_ld(x[0]);
                     tmem_waited(x[1]);
-                    const bool edge = key0 + kTileKeys > all_see;  // some row of the warp does not see the whole tile
+                    const bool edge = key0 > whole_to;  // some row of the warp does not see the whole tile
                     unsigned long long seen = ~0ull;
                     if (edge) {
                         seen = seen_columns(upto - key0, nodes, p.base + 1 - key0);
@@ -814,7 +815,7 @@ attn_tile_kernel(const AttnArgs a, const Work ws, const Geometry g, const int bo
                     }
                 }
                 if (valid && *static_cast<volatile int*>(&sh.not_finite[items % kFlags])) {
-                    const int lo = max(item_sees, p.kv0 * kTileKeys), hi = min(p.kv1 * kTileKeys, kv_end);
+                    const int lo = max(item_sees, p.kv0 * kTileKeys), hi = p.kv1 == p.nkv ? kv_end : p.kv1 * kTileKeys;
                     restore_cleared<E>(a, p.b, p.h, lo, hi, upto, nodes, p.base + 1, c_lo, min(c_hi, a.head_dim), whole ? out : nullptr, po);
                 }
             }

@@ -435,6 +435,24 @@ def test_page_entries_outside_the_pool_stand_for_zeros():
     R.check_attention(p, out, lse, R.attention(p, kd=kd, vd=vd))
 
 
+def test_a_cache_that_ends_in_the_last_tile_below_2_to_31():
+    """Every page of the table but the last is the same one; keys of zeros, values of ones.  What lies behind the last token is NaN."""
+    import paper_2606_01019_b200 as H
+    page, width = 65528, 32772
+    end = page * width - 4
+    k, v = torch.zeros(2, page, 1, 8, dtype=BF, device="cuda"), torch.ones(2, page, 1, 8, dtype=BF, device="cuda")
+    k[1, -4:], v[1, -4:] = float("nan"), float("nan")
+    table = torch.zeros(1, width, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    ctx = H.Context(max_batch=1, k_cap=1, max_hist_len=16, max_rows=1, max_vocab=8)
+    ctx.hvd_set_attention(n_q_heads=1, n_kv_heads=1, head_dim=8)
+    q, out, lse = torch.ones(1, 1, 8, dtype=BF, device="cuda"), torch.empty(1, 1, 8, dtype=BF, device="cuda"), torch.empty(1, 1, device="cuda")
+    ctx.hvd_attn_paged(1, H.KvCache(k, v, table), torch.tensor([end - 1], dtype=torch.int32, device="cuda"), None, 0, 1, None, None, q, out, lse)
+    assert (out == 1).all() and abs(float(lse) - np.log(end)) < 1e-5
+    assert ctx.hvd_device_status() == 0
+    ctx.close()
+
+
 def test_long_ragged_batch_split_over_the_sms():
     """Contexts from one token to 40 000: most are cut into pieces that are joined again."""
     rng = np.random.default_rng(8)
