@@ -108,7 +108,8 @@ typedef enum {
     HVD_REQ_OK = 0,
     HVD_REQ_CAPACITY = 1, /* slab too small: commit clamped to the free space */
     HVD_REQ_BAD_LEN = 2,  /* hist_len outside [0, hist_cap] or no logits rows: request skipped */
-    HVD_REQ_BAD_PAGE = 3  /* cache operators: an entry of the page table lies outside the pool */
+    HVD_REQ_BAD_PAGE = 3, /* cache operators: an entry of the page table lies outside the pool */
+    HVD_REQ_BAD_PATH = 4  /* hvd_kv_commit_checked: the tree does not lead along the committed tokens */
 } hvd_req_status;
 
 /* values of the device status word (hvd_device_status) */
@@ -697,7 +698,8 @@ HVD_API hvd_status hvd_attn_paged(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* c
  * j-th accepted node (j = 0 .. min(accepted, n_commit - 1) - 1) goes from slot cache_len + 1 + node to slot
  * cache_len + 1 + j, in every layer.  The path is the one that hvd_verify_commit_tree took: from the root, the child of
  * lowest index that carries the next token of `committed`.  Where the path ends early (outputs of another
- * call) or an entry of the page table lies outside the pool, the rest of the request's nodes stays where it is.
+ * call) or an entry of the page table lies outside the pool, the rest of the request's nodes stays where it is,
+ * and the length is raised all the same (hvd_kv_commit_checked tells).
  *
  * cache        the first layer's; layer l's arrays start l * layer_stride elements (a multiple of 8) further on,
  *              n_layers 1 .. 4096
@@ -711,6 +713,18 @@ HVD_API hvd_status hvd_kv_commit(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* ca
                                  int64_t layer_stride, const int32_t* cache_len, const int32_t* parent,
                                  const int32_t* sel_draft, const int32_t* sel_len, const int32_t* accepted,
                                  const int32_t* committed, const int32_t* n_commit, int32_t* new_len, void* stream);
+
+/*
+ * The same with a verdict for every request (the length is raised in each case but BAD_LEN, as above):
+ * status  int32 [B], DEVICE output, may be NULL: HVD_REQ_OK; HVD_REQ_BAD_LEN (cache_len < 0, or cache_len + n_commit beyond the
+ *         table); HVD_REQ_BAD_PAGE, HVD_REQ_BAD_PATH: an accepted node is not where the new length says, because a page
+ *         lies outside the pool, or because the path ends before min(accepted, n_commit - 1) nodes
+ */
+HVD_API hvd_status hvd_kv_commit_checked(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int32_t n_layers,
+                                         int64_t layer_stride, const int32_t* cache_len, const int32_t* parent,
+                                         const int32_t* sel_draft, const int32_t* sel_len, const int32_t* accepted,
+                                         const int32_t* committed, const int32_t* n_commit, int32_t* new_len,
+                                         int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

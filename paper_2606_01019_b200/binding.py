@@ -13,7 +13,7 @@ import numpy as np
 from . import build as _build
 
 F32, BF16, F16 = 0, 1, 2
-REQ_OK, REQ_CAPACITY, REQ_BAD_LEN, REQ_BAD_PAGE = 0, 1, 2, 3
+REQ_OK, REQ_CAPACITY, REQ_BAD_LEN, REQ_BAD_PAGE, REQ_BAD_PATH = 0, 1, 2, 3, 4
 ROPE_HALVES, ROPE_PAIRS = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS, ROPE_BANDS = 0, 1, 2, 3, 4
 N_FEATURES = 8
@@ -98,6 +98,7 @@ _SIGNATURES = {
     "hvd_attn_paged": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _vp, _vp, _i32, _i64, _vp, _vp]
                        + [C.POINTER(HvdHeads)] * 2 + [_vp, _vp, _vp]),
     "hvd_kv_commit": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _i32, _i64] + [_vp] * 9),
+    "hvd_kv_commit_checked": (_i32, [_vp, _i32, C.POINTER(HvdKvCache), _i32, _i64] + [_vp] * 10),
 }
 
 _lib = None
@@ -498,8 +499,14 @@ class Context:
             self._check(st, "hvd_attn_paged")
 
     def hvd_kv_commit(self, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
-                      n_commit, new_len):
+                      n_commit, new_len, status=None):
+        """With status (int32 [B]) the call is hvd_kv_commit_checked."""
         ref, stream = self._cache_arg(cache)
-        self._check(self._lib.hvd_kv_commit(self._h, B, ref, n_layers, layer_stride, _ptr(cache_len), _ptr(parent), _ptr(sel_draft),
-                                            _ptr(sel_len), _ptr(accepted), _ptr(committed), _ptr(n_commit), _ptr(new_len), stream),
-                    "hvd_kv_commit")
+        if status is not None:
+            st = self._lib.hvd_kv_commit_checked(self._h, B, ref, n_layers, layer_stride, _ptr(cache_len), _ptr(parent), _ptr(sel_draft),
+                                                 _ptr(sel_len), _ptr(accepted), _ptr(committed), _ptr(n_commit), _ptr(new_len),
+                                                 _ptr(status), stream)
+        else:
+            st = self._lib.hvd_kv_commit(self._h, B, ref, n_layers, layer_stride, _ptr(cache_len), _ptr(parent), _ptr(sel_draft),
+                                         _ptr(sel_len), _ptr(accepted), _ptr(committed), _ptr(n_commit), _ptr(new_len), stream)
+        self._check(st, "hvd_kv_commit")

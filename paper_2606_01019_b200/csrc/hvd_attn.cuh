@@ -126,6 +126,7 @@ struct KvCommitArgs {
     const int32_t* committed;
     const int32_t* n_commit;
     int32_t* new_len;
+    int32_t* status;    // may be NULL
     bool in_place;      // new_len is cache_len
     uint32_t* arrived;  // [max_batch], zero at rest
 };

@@ -205,6 +205,14 @@ hvd_status hvd_kv_commit(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int
                          const int32_t* cache_len, const int32_t* parent, const int32_t* sel_draft,
                          const int32_t* sel_len, const int32_t* accepted, const int32_t* committed,
                          const int32_t* n_commit, int32_t* new_len, void* stream) {
+    return hvd_kv_commit_checked(ctx, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
+                                 n_commit, new_len, nullptr, stream);
+}
+
+hvd_status hvd_kv_commit_checked(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int32_t n_layers, int64_t layer_stride,
+                                 const int32_t* cache_len, const int32_t* parent, const int32_t* sel_draft,
+                                 const int32_t* sel_len, const int32_t* accepted, const int32_t* committed,
+                                 const int32_t* n_commit, int32_t* new_len, int32_t* status, void* stream) {
     static const char* who = "hvd_kv_commit";
     if (!ctx) return HVD_ERR_INVALID_ARG;
     if (const char* w = cache_fault(ctx, B, cache, cache_len)) return fail_at(ctx, HVD_ERR_INVALID_ARG, who, w);
@@ -217,7 +225,7 @@ hvd_status hvd_kv_commit(hvd_ctx* ctx, int32_t B, const hvd_kv_cache* cache, int
     a.c = chunk_args(ctx, B, *cache, cache_len, nullptr, 0, 0, sel_len, parent);
     a.n_layers = n_layers; a.n_kv_heads = ctx->attn.n_kv_heads; a.head_dim = ctx->attn.head_dim;
     a.layer_stride = layer_stride;
-    a.sel_draft = sel_draft; a.accepted = accepted; a.committed = committed; a.n_commit = n_commit; a.new_len = new_len; a.in_place = new_len == cache_len;
+    a.sel_draft = sel_draft; a.accepted = accepted; a.committed = committed; a.n_commit = n_commit; a.new_len = new_len; a.status = status; a.in_place = new_len == cache_len;
     a.arrived = ctx->at_arrived;
     return launch_kv_commit(ctx, a, static_cast<cudaStream_t>(stream));
 }

@@ -14,6 +14,8 @@ namespace {
 constexpr int kKvThreads = 256;
 constexpr uint32_t kFull = 0xffffffffu;
 
+// VERDICT: with a status for every request (0.15 us of 5.8; without it the code is left out)
+template <bool VERDICT>
 __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArgs a) {
     __shared__ int64_t from[kTreeRows], to[kTreeRows];
     __shared__ int n_moves, new_length;
@@ -27,7 +29,7 @@ __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArg
         // all loads that hang on nothing at once
         const int base = c.cache_len[b];
         const int w = a.n_commit[b];
-        int m = 0, most = 0, dt[2] = {-1, -1}, pr[2] = {-2, -2}, zt[2] = {-1, -1};
+        int m = 0, wanted = 0, most = 0, dt[2] = {-1, -1}, pr[2] = {-2, -2}, zt[2] = {-1, -1};
         if (c.parent) {
             m = c.sel_len[b];
             most = a.accepted[b];
@@ -41,9 +43,11 @@ __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArg
                 }
             }
             m = max(0, min(m, kc));
-            most = min(min(most, w - 1), m);
+            wanted = min(most, w - 1);
+            most = min(wanted, m);
         }
         const bool usable = w > 0 && base >= 0 && (int64_t)base + w <= (int64_t)c.table_stride * c.page_size;
+        int status = usable || (w <= 0 && base >= 0 && base <= (int64_t)c.table_stride * c.page_size) ? HVD_REQ_OK : HVD_REQ_BAD_LEN;
         const int len = usable ? base + w : base;
         if (lane == 0) {
             new_length = len;
@@ -81,12 +85,17 @@ __global__ void __launch_bounds__(kKvThreads) kv_commit_kernel(const KvCommitArg
             const int end = f0 ? __ffs(f0) - 1 : (f1 ? 32 + __ffs(f1) - 1 : steps);
             const uint32_t m0 = __ballot_sync(kFull, lane < end && src[0] != lane);
             const uint32_t m1 = __ballot_sync(kFull, lane + 32 < end && src[1] != lane + 32);
+            if (VERDICT && end < steps) status = HVD_REQ_BAD_PAGE;
+            else if (VERDICT && steps < wanted) status = HVD_REQ_BAD_PATH;
             const uint32_t below = (1u << lane) - 1u;
             if ((m0 >> lane) & 1u) { const int s = __popc(m0 & below); from[s] = fo[0]; to[s] = ta[0]; }
             if ((m1 >> lane) & 1u) { const int s = __popc(m0) + __popc(m1 & below); from[s] = fo[1]; to[s] = ta[1]; }
             moves = __popc(m0) + __popc(m1);
         }
-        if (lane == 0) n_moves = moves;
+        if (lane == 0) {
+            n_moves = moves;
+            if (VERDICT && blockIdx.y == 0) a.status[b] = status;
+        }
     }
     __syncthreads();
     const int n = n_moves;
@@ -124,8 +133,8 @@ hvd_status launch_kv_commit(hvd_ctx* ctx, const KvCommitArgs& a, cudaStream_t st
     const int64_t vecs = (int64_t)a.n_layers * 2 * a.n_kv_heads * (a.head_dim / 8);
     int64_t gy = a.c.parent ? (vecs + kKvThreads - 1) / kKvThreads : 1;
     if (gy > 1024) gy = 1024;
-    const cudaError_t e = launch_kernel((ctx->pdl_mask & 16) != 0, kv_commit_kernel, dim3((unsigned)a.c.B, (unsigned)gy),
-                                        dim3(kKvThreads), 0, stream, a);
+    const cudaError_t e = launch_kernel((ctx->pdl_mask & 16) != 0, a.status ? kv_commit_kernel<true> : kv_commit_kernel<false>,
+                                        dim3((unsigned)a.c.B, (unsigned)gy), dim3(kKvThreads), 0, stream, a);
     return e == cudaSuccess ? HVD_OK : cuda_fail(ctx, e, "kv_commit_kernel");
 }
 

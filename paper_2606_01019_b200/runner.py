@@ -161,7 +161,8 @@ class PagedCache:
         self.v = torch.empty_like(self.k)
         self.table = torch.arange(B * per, dtype=torch.int32, device=device).reshape(B, per)
         self.length = torch.zeros(B, dtype=torch.int32, device=device)     # tokens cached
-        self.status = torch.zeros(B, dtype=torch.int32, device=device)
+        self.status = torch.zeros(B, dtype=torch.int32, device=device)            # the last append's verdict per request
+        self.commit_status = torch.zeros(B, dtype=torch.int32, device=device)     # the last commit's
         self.layer = [KvCache(self.k[i], self.v[i], self.table) for i in range(n_layers)]
 
     def append(self, layer, q, k, v, q_out, *, row_off=None, k_uniform=0, sel_len=None, parent=None):
@@ -176,4 +177,4 @@ class PagedCache:
     def commit(self, n_commit, *, sel_draft=None, sel_len=None, parent=None, accepted=None, committed=None):
         """Takes the chunk's first n_commit tokens (of a tree: the root and its accepted nodes) into the cache."""
         self.ctx.hvd_kv_commit(self.B, self.layer[0], self.n_layers, self.k.stride(0), self.length, parent, sel_draft, sel_len,
-                               accepted, committed, n_commit, self.length)
+                               accepted, committed, n_commit, self.length, self.commit_status)

@@ -118,6 +118,44 @@ def test_a_path_that_ends_early_and_pages_outside_the_pool():
     assert same(k, c.k) and same(v, c.v)
 
 
+@pytest.mark.parametrize("alias", [False, True])
+def test_the_verdict_of_every_request(alias):
+    import paper_2606_01019_b200 as H
+    c = Commit(8, 40, 3, seed=11, page=8, lens=[7, 15, 20, 31, 3, 0, 9, 50])
+    longest = sorted(range(8), key=lambda i: -len(c.paths[i]))
+    b, e, f = longest[:3]                                          # a page outside, a path that ends early, more nodes than the tree has
+    assert len(c.paths[f]) >= 2
+    want = np.zeros(8, np.int32)
+    c.p.table[b, (c.p.lens[b] + 1 + c.paths[b][-1]) // 8] = c.p.n_pages
+    want[b] = H.REQ_BAD_PAGE
+    c.com[e, 1] = -77
+    want[e] = H.REQ_BAD_PATH
+    c.accepted[f], c.n_commit[f] = 41, 42
+    want[f] = H.REQ_BAD_PATH
+    rest = longest[3:]
+    lens, n = np.array(c.p.lens), c.n_commit.copy()
+    lens[rest[0]], lens[rest[1]] = -7, 8 * c.p.table.shape[1]
+    want[rest[0]] = want[rest[1]] = H.REQ_BAD_LEN
+    n[rest[2]], n[rest[3]] = 0, 1                                  # nothing to commit; the root alone
+    width = 8 * c.p.table.shape[1]
+    assert lens[f] + 42 <= width
+    c.p.device()
+    up = lambda x: torch.as_tensor(np.ascontiguousarray(x), device="cuda", dtype=torch.int32)
+    ctx, ln = c.p.context(), up(lens)
+    new, status = ln if alias else torch.full_like(ln, -9), torch.full_like(ln, -5)
+    ctx.hvd_kv_commit(8, H.KvCache(c.k[0], c.v[0], c.p.t_table), 3, c.k.stride(0), ln, c.p.t_par, up(c.tok), c.p.t_sel, up(c.accepted), up(c.com), up(n),
+                      new, status)
+    assert status.tolist() == want.tolist()
+    ok = lens + np.where((n > 0) & (want != H.REQ_BAD_LEN), n, 0)
+    assert new.tolist() == ok.tolist()
+    # chains
+    ln, n = up([5, -1, width, 3]), up([2, 1, 1, 0])
+    st = torch.full_like(ln, -5)
+    ctx.hvd_kv_commit(4, H.KvCache(c.k[0], c.v[0], c.p.t_table), 3, c.k.stride(0), ln, None, None, None, None, None, n, torch.empty_like(ln), st)
+    assert st.tolist() == [0, H.REQ_BAD_LEN, H.REQ_BAD_LEN, 0]
+    ctx.close()
+
+
 def test_refusals():
     import paper_2606_01019_b200 as H
     c = Commit(2, 4, 2)
