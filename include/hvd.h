@@ -645,9 +645,10 @@ typedef struct {
    factor on cos and sin in *magnitude.  HVD_ERR_INVALID_ARG if cfg is not one that hvd_set_attention takes. */
 HVD_API hvd_status hvd_rope_frequencies(const hvd_attn_config* cfg, double* freq, double* magnitude);
 
-/* Stores the attention geometry and allocates the operators' scratch (partial results of rows whose keys are
-   split over several SMs: two slots of 256 rows per SM, about 39 MB at head_dim 128).  A set-up call: it
-   waits for the device and is not for stream capture; no operator of this context may be in flight. */
+/* Stores the attention geometry and, the first time, allocates the operators' scratch (partial results of rows whose keys are
+   split over several SMs: two slots of 256 rows per SM, about 39 MB).  A set-up call: it waits for the device and is not
+   for stream capture; no operator of this context may be in flight.  Graphs keep the geometry under which they were
+   captured, but turn by the frequencies that are set when they run. */
 HVD_API hvd_status hvd_set_attention(hvd_ctx* ctx, const hvd_attn_config* cfg);
 
 /*

@@ -130,16 +130,11 @@ hvd_status hvd_set_attention(hvd_ctx* ctx, const hvd_attn_config* cfg) {
     HVD_CUDA_TRY(ctx, cudaDeviceSynchronize());
     const hvd_status st = attn_setup(ctx);
     if (st != HVD_OK) return st;
-    const size_t bytes = attn_workspace_bytes(ctx->num_sms, cfg->head_dim);
-    if (bytes > ctx->at_ws_bytes) {
-        cudaFree(ctx->at_ws);
+    // once, for the widest heads: graphs that were captured under an earlier geometry hold its address
+    if (!ctx->at_ws && cudaMalloc(&ctx->at_ws, attn_workspace_bytes(ctx->num_sms, HVD_MAX_HEAD_DIM)) != cudaSuccess) {
         ctx->at_ws = nullptr;
-        ctx->at_ws_bytes = 0;
-        if (cudaMalloc(&ctx->at_ws, bytes) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return fail(ctx, HVD_ERR_ALLOC, "hvd_set_attention: out of device memory for the scratch");
-        }
-        ctx->at_ws_bytes = bytes;
+        (void)cudaGetLastError();
+        return fail(ctx, HVD_ERR_ALLOC, "hvd_set_attention: out of device memory for the scratch");
     }
     if (!ctx->at_turns) HVD_CUDA_TRY(ctx, cudaMalloc(&ctx->at_turns, sizeof(turns)));
     HVD_CUDA_TRY(ctx, cudaMemcpy(ctx->at_turns, turns, sizeof(turns), cudaMemcpyHostToDevice));

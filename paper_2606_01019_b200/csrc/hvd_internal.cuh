@@ -111,7 +111,6 @@ struct hvd_ctx {
     bool has_attention;
     unsigned long long* at_turns;    // [HVD_MAX_HEAD_DIM / 2] angular frequencies in 2^-64 turns per position
     void* at_ws;                     // attention: partial sums of items that several SMs share
-    size_t at_ws_bytes;
     uint32_t* at_arrived;            // [max_batch] zero at rest: CTAs of a request that have read its length
     char last_error[256];
 };

@@ -501,6 +501,29 @@ def test_another_stream_and_a_graph():
     ctx.close()
 
 
+def test_a_graph_outlives_another_geometry():
+    """A graph captured with heads of 64 runs after the context has been set to heads of 128 and used with them."""
+    p = R.Problem(lens=[3000, 1300], rows=[9, 9], hq=8, hkv=2, d=64, page=16, seed=26).fill().device()
+    wide = R.Problem(lens=[3000, 1300], rows=[9, 9], hq=8, hkv=2, d=128, page=16, seed=27).fill()
+    ctx, cache, out, lse = p.context(), p.cache(), torch.zeros_like(p.q), torch.zeros(p.total, p.hq, device="cuda")
+    call = lambda: ctx.hvd_attn_paged(p.B, cache, p.t_len, p.t_off, 0, p.total, None, None, p.q, out, lse)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    ctx.hvd_set_attention(n_q_heads=8, n_kv_heads=2, head_dim=128)
+    R.check_attention(wide, *run(wide, ctx=ctx), R.attention(wide))
+    filler = torch.full((48 << 20,), 0x7f, dtype=torch.uint8, device="cuda")
+    out.zero_(), lse.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    R.check_attention(p, out, lse, R.attention(p))
+    assert (filler == 0x7f).all()
+    del g
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 2^32 bytes and 2^31 elements per array; the request's pages lie at its end."""
     p = R.Problem(lens=[500], rows=[5], hq=4, hkv=2, d=128, page=64, seed=14, pool_pages=(1 << 31) // (64 * 256) + 64)
