@@ -177,10 +177,12 @@ class KvCache:
             raise HvdError("KvCache: k and v are tensors [n_pages, page_size, n_kv_heads, head_dim] of one type, shape and layout")
         if k.stride(3) != 1 and k.shape[3] > 1:
             raise HvdError("KvCache: the elements of a head must be contiguous")
+        if not (k.is_cuda and v.is_cuda and page_table.is_cuda):
+            raise HvdError("KvCache: k, v and page_table are CUDA tensors")
         if page_table.dim() != 2 or not page_table.is_contiguous() or str(page_table.dtype) != "torch.int32":
             raise HvdError("KvCache: page_table is a contiguous int32 tensor [B, pages]")
         self.k, self.v, self.page_table = k, v, page_table
-        self.heads, self.type = (k.shape[2], k.shape[3]), k.dtype
+        self.heads, self.type, self.requests = (k.shape[2], k.shape[3]), k.dtype, page_table.shape[0]
         self._c = HvdKvCache(_ptr(k), _ptr(v), k.shape[0], k.shape[1], page_table.shape[1], _ptr(page_table),
                              _step(k, 0), _step(k, 1), _step(k, 2))
         self._ref = C.byref(self._c)
@@ -463,10 +465,12 @@ class Context:
         h.head_stride = head if heads > 1 else d
         return self._arg_ref[i]
 
-    def _cache_arg(self, cache):
+    def _cache_arg(self, cache, B):
         """The cache's struct and the current stream, once the geometry is set (the library refuses the call otherwise)."""
         if self.attn is None:
             return cache._ref, None
+        if B > cache.requests and B <= self.cfg.max_batch:      # beyond max_batch the library refuses
+            raise HvdError(f"the page table has {cache.requests} requests, the call {B}")
         _, nkv, d, dtype = self._geometry
         if cache.heads != (nkv, d):
             raise HvdError("the cache has other heads than hvd_set_attention was given")
@@ -475,7 +479,7 @@ class Context:
         return cache._ref, self._raw_stream(self._dev)
 
     def hvd_rope_append(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, k, v, q_out, status):
-        ref, stream = self._cache_arg(cache)
+        ref, stream = self._cache_arg(cache, B)
         nq, nkv = self._geometry[:2]
         h = self._heads_arg
         st = self._lib.hvd_rope_append(
@@ -488,8 +492,10 @@ class Context:
 
     def hvd_attn_paged(self, B, cache, cache_len, row_off, k_uniform, total_rows, sel_len, parent, q, out, lse=None,
                        status=None):
-        ref, stream = self._cache_arg(cache)
+        ref, stream = self._cache_arg(cache, B)
         nq = self._geometry[0]
+        if lse is not None and (lse.numel() < total_rows * nq or lse.element_size() != 4 or not lse.is_contiguous()):
+            raise HvdError(f"lse is a contiguous float32 tensor [total_rows, {nq}]")
         st = self._lib.hvd_attn_paged(
             self._h, B, ref, cache_len.data_ptr(), None if row_off is None else row_off.data_ptr(), k_uniform, total_rows,
             None if sel_len is None else sel_len.data_ptr(), None if parent is None else parent.data_ptr(),
@@ -501,7 +507,7 @@ class Context:
     def hvd_kv_commit(self, B, cache, n_layers, layer_stride, cache_len, parent, sel_draft, sel_len, accepted, committed,
                       n_commit, new_len, status=None):
         """With status (int32 [B]) the call is hvd_kv_commit_checked."""
-        ref, stream = self._cache_arg(cache)
+        ref, stream = self._cache_arg(cache, B)
         if status is not None:
             st = self._lib.hvd_kv_commit_checked(self._h, B, ref, n_layers, layer_stride, _ptr(cache_len), _ptr(parent), _ptr(sel_draft),
                                                  _ptr(sel_len), _ptr(accepted), _ptr(committed), _ptr(n_commit), _ptr(new_len),

@@ -596,6 +596,31 @@ def test_refusals():
     ctx.close()
 
 
+def test_arrays_too_small_for_the_call_are_refused():
+    import paper_2606_01019_b200 as H
+    p = R.Problem(lens=[20, 9], rows=[4, 4], hq=4, hkv=2, d=64, page=16).fill().device()
+    ctx, out = p.context(), torch.zeros_like(p.q)
+    lse = torch.zeros(p.total, p.hq, device="cuda")
+    short = H.KvCache(p.k, p.v, p.t_table[:1].contiguous())
+    attn = lambda cache, lse: ctx.hvd_attn_paged(2, cache, p.t_len, p.t_off, 0, p.total, None, None, p.q, out, lse)
+    with pytest.raises(H.HvdError, match="page table has 1"):
+        attn(short, lse)
+    kv = torch.zeros(p.total, 2, 64, dtype=BF, device="cuda")
+    with pytest.raises(H.HvdError, match="page table has 1"):
+        ctx.hvd_rope_append(2, short, p.t_len, p.t_off, 0, p.total, None, None, p.q, kv, kv, out, p.status)
+    with pytest.raises(H.HvdError, match="page table has 1"):
+        ctx.hvd_kv_commit(2, short, 1, 0, p.t_len, None, None, None, None, None, p.t_len, torch.empty_like(p.t_len))
+    for bad in (lse[:-1], lse.half(), torch.zeros(p.total, 2 * p.hq, device="cuda")[:, ::2]):
+        with pytest.raises(H.HvdError, match="lse is a contiguous"):
+            attn(p.cache(), bad)
+    for i in range(3):
+        with pytest.raises(H.HvdError, match="CUDA tensors"):
+            H.KvCache(*[t.cpu() if i == j else t for j, t in enumerate((p.k, p.v, p.t_table))])
+    attn(p.cache(), lse)
+    R.check_attention(p, out, lse, R.attention(p))
+    ctx.close()
+
+
 def _again(env, select):
     import os
     import subprocess
