@@ -655,8 +655,8 @@ HVD_API hvd_status hvd_set_attention(hvd_ctx* ctx, const hvd_attn_config* cfg);
  * Rotary positions and cache append.  For every new token (row i of the chunk, position
  * t = cache_len[b] + i, or + the node's depth in a tree): with a = t * w_j, (c, s) = rope_magnitude * (cos a, sin a),
  * each rotated pair (x, y) of its q and k heads becomes (x c - y s, x s + y c); the other elements stay as they are.
- * q goes to q_out, k and v to the token's cache slot.  Angles are right to 2^-26 of a turn at every position;
- * the products are in 32 bits and rounded once.  Rows that are no new token are not written.
+ * q goes to q_out, k and v to the token's cache slot.  Angles are right to 2^-25 of a turn at positions up to 2^27, to 2^-23 beyond,
+ * of the frequencies that hvd_rope_frequencies gives (64-bit floats); the products are in 32 bits and rounded once.  Rows that are no new token are not written.
  * A token whose page entry lies outside [0, n_pages) is not cached: status HVD_REQ_BAD_PAGE (its q_out is written).
  *
  * q, k, v  HOST structs: [total_rows] rows of n_q_heads, n_kv_heads, n_kv_heads heads

@@ -20,10 +20,11 @@
 // several CTAs share leaves partial sums, which attn_finish_kernel joins in the order of the CTAs: no result depends on
 // timing.
 //
-// Measured on one B200, calls in a row in a graph: 64 requests of 16 K tokens with 17 rows, 32/8 heads of 128: 681 us for 4.3 GB of keys
-// and values (6.3 TB/s, bound by HBM); 96 ragged requests, one row: 491 us (6.2 TB/s); 4 x 2047 rows behind 1.5 to 9 K tokens: 715 us
-// (971 TFLOP/s; bound by the alternation of products and softmax: 1860 cycles a pair of steps, the products alone 1285); one token
-// behind 1037: 13.6 us (two launches and their round trips).  Key tiles of 64 instead of 128: with 128 a stream's scores, weights and sums
+// Measured on one B200, in graphs of a few milliseconds / in long runs, which the power limit slows down: 64 requests of 16 K tokens with 17
+// rows, 32/8 heads of 128: 666 / 797 us for 4.3 GB of keys and values (6.5 / 5.4 TB/s, bound by HBM, then by power); 96 ragged requests, one
+// row: 484 / 541 us (6.3 / 5.6 TB/s); 4 x 2047 rows behind 1.5 to 9 K tokens: 681 / 790 us (1019 / 879 TFLOP/s; bound by the alternation
+// of products and softmax: 1860 cycles a pair of steps, the products alone 1285); one token behind 1037: 13.6 / 13.9 us (two launches
+// and their round trips).  Key tiles of 64 instead of 128: with 128 a stream's scores, weights and sums
 // leave no room for a second buffer, and six tiles in flight hide HBM better than two and a half (one-token decode 104 -> 93 us).
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>

@@ -4,7 +4,7 @@
 // slot j: a thread that owns one 16-byte column of the cache rows may read any later source before it writes an
 // earlier target, and the moves of a request need no copy aside.  Bound by the bytes moved and by the two or three dependent
 // global round trips at the start (lengths, tree, page table): 16 trees in 16 layers 3.7 us, 128 trees in 32 layers (10 MB read and written)
-// 6.3 us.
+// 6.3 us; with the length raised in place, which takes a counter per request, 1.1 and 1.6 us more.
 #include "hvd_attn.cuh"
 
 namespace hvd {

@@ -1,8 +1,10 @@
 // hvd_rope_append: rotary positions on the new tokens' queries and keys, keys and values into the paged cache.
 //
 // A pair (x, y) of a head turns by the angle a = t * w at position t.  The frequency is held in units of 2^-64
-// turns, so that t * w modulo one turn is an integer product that wraps: exact at every position, where a
-// 32-bit float product is off by thousandths of a radian from position 10^5 on.  The upper 32 bits go to sincospi.
+// turns, so that t * w modulo one turn is an integer product that wraps, exact for the frequency as held, where a
+// 32-bit float product is off by thousandths of a radian from position 10^5 on.  The upper 32 bits go to sincospi.  (The frequency
+// comes through 64-bit floats, good to 2^-52 of itself, and the angle is rounded to 24 bits of half a turn: together 2^-25 of a
+// turn at positions up to 2^27, 2^-23 at 2^31.)
 //
 // Bandwidth: every element is read once and written once.  A CTA takes a few tokens.  Where a token goes hangs on four or five global
 // round trips (request, lengths, page), so the rows themselves, which hang on none, are asked for first and wait in registers;
